@@ -13,7 +13,8 @@
  *     where stated; nothing throws or aborts.
  *   - rnnlm_load takes HOST pointers and copies; the caller keeps its buffers.
  *   - rnnlm_dedup / rnnlm_step / rnnlm_step_dedup / rnnlm_step_cached / rnnlm_pack_ids /
- *     rnnlm_index_intern / rnnlm_index_fetch / rnnlm_hs_step take
+ *     rnnlm_index_intern / rnnlm_index_fetch / rnnlm_hs_step / rnnlm_q4_matvec / rnnlm_sample /
+ *     rnnlm_distill / rnnlm_distill_backward take
  *     DEVICE pointers owned by the caller and are asynchronous on `hip_stream` (a
  *     hipStream_t passed as void*; NULL = the default stream).  No call here synchronises,
  *     allocates or frees device memory except rnnlm_load, rnnlm_hs_load, rnnlm_free, rnnlm_last_error,
@@ -360,6 +361,113 @@ int rnnlm_index_stats(rnnlm_index_table *table, void *hip_stream, int64_t out[6]
  */
 int rnnlm_pack_ids(const uint32_t *ctx_idx, const uint32_t *small_lm_idx, int N, uint64_t *ids,
                    void *hip_stream);
+
+/*
+ * ---- Answering and learning: rows of logits from 4-bit weights, the next word, a teacher's top logits ----
+ *
+ * The step above gives the few log-probabilities a search asks for.  A program that writes text with a model, or trains a
+ * smaller one for a search from a larger one, needs whole rows of logits, a word drawn from each, and the loss of a row
+ * with its gradient.  These entry points take no model handle: all pointers except rnnlm_q4_quantize's are DEVICE pointers
+ * owned by the caller, calls are asynchronous on `hip_stream`, allocate nothing and may be captured into a HIP graph.
+ * Element types are rnnlm_dtype; a row stride (`ld`) counts elements from one row to the next and is at least the row's
+ * length.  Outputs must not share a byte with inputs or with each other (RNNLM_EINVAL) unless stated.
+ * A workspace is scratch: contents undefined before and after, 16-byte aligned, one per call that may be in flight.
+ */
+
+/*
+ * Rows of logits (or any linear layer) from weights of 4 bits in groups with a scale each:
+ *   y[b][v] = bias[v] + sum_g scale[g][v] * sum_{j in group g} (code[v][j] - zero[g][v]) x[b][j],   groups g = j / group
+ *   codes   dev u8[V][code_ld]  two codes of 0..15 a byte, the even unit j in the low four bits; row v starts at byte
+ *                               v * code_ld, any code_ld >= ceil(H / 2) and any alignment (rows that start at multiples of 16
+ *                               bytes are read fastest); the high half of the last byte of an odd H is ignored
+ *   group                       32, 64 or 128 units (the last group of a row may be shorter)
+ *   scale   dev [ceil(H / group)][V]  float or bfloat16 (scale_dtype)
+ *   zero    dev u8[ceil(H / group)][V] with values 0..255, or NULL: 8 everywhere
+ *   bias    dev f32[V] or NULL: 0
+ *   x       dev [B][x_ld]  float or bfloat16;  y  dev [B][y_ld] float or bfloat16 (out), any pair of types
+ * Codes less their zero are exact; an fp32 x is taken as two fp16 terms relative to its row's largest finite magnitude (good to
+ * 2^-23 of itself or 2^-39 of that magnitude, whichever is larger); sums are held in fp32, and y is rounded once at the end.
+ * An x that is infinite or NaN reaches the outputs of its row as in exact arithmetic (infinity times a zero weight is NaN),
+ * and no other row.  B = 0 is a no-op.  H <= 65536, V <= 2^30.
+ */
+int rnnlm_q4_matvec(int B, int V, int H, int group, const uint8_t *codes, long long code_ld, int scale_dtype, const void *scale,
+                    const uint8_t *zero_or_null, const float *bias_or_null, int x_dtype, const void *x, long long x_ld,
+                    int y_dtype, void *y, long long y_ld, void *hip_stream);
+
+/*
+ * Codes, scales and zero points for rnnlm_q4_matvec from float weights w[V][H] (HOST arrays, host code), each group by itself:
+ * with zero == NULL  scale = (largest magnitude) / 7, code = 8 + round(w / scale), within 1..15;
+ * else               scale = (max(w, 0) - min(w, 0)) / 15, zero = round(-min / scale), code = zero + round(w / scale), within 0..15.
+ * Rounding is to nearest, ties to even.  A group of zeros gets scale 0 and codes equal to its zero point.
+ *   codes  out u8[V][ceil(H / 2)] (the free half of an odd row's last byte is 0);  scale  out f32[ceil(H / group)][V];
+ *   zero   out u8[ceil(H / group)][V] or NULL
+ * RNNLM_EINVAL for weights that are not finite.
+ */
+int rnnlm_q4_quantize(int V, int H, int group, const float *w, uint8_t *codes, float *scale, uint8_t *zero_or_null);
+
+/* Bytes of workspace rnnlm_sample needs (0 for N <= 0 or V <= 0). */
+size_t rnnlm_sample_workspace_bytes(int N, int V);
+
+/*
+ * One word from each of N rows of logits by given uniform numbers.  Row n, with y_i = (z_i - max z) / temperature and
+ * w_i = exp(y_i); words stand in the order of falling logits, equal ones by rising id:
+ *   top_k  keeps the first top_k words (0 or less, or V and more: all);
+ *   top_p  then keeps the shortest run from the front whose weights add up to at least top_p of what top_k left (1 and more:
+ *          all; 0 and less: the first word);
+ *   min_p  then keeps words with w_i >= min_p (a share of the most probable word's; 0 and less: all, 1 and more: those as
+ *          probable as the most probable one);
+ *   word[n] = the smallest id i, among the words kept, with (sum of w_j kept, j <= i) > u[n] * (sum of all w_j kept),
+ *   logprob[n] = log(w_word / sum of all w_j kept).
+ * temperature 0: the first word of the order, logprob 0.  Logits of -infinity are words that cannot come; where some are
+ * +infinity, those share the row equally.  A row without any word (all -infinity), with a NaN, or with a
+ * temperature that is negative or not finite, u outside [0, 1), or top_p or min_p NaN gets word -1 and logprob NaN.
+ * Weights are fixed-point numbers of 62 - ceil(log2 V) fractional bits, computed in 64 bits and added exactly: the word
+ * does not depend on how the work is split.  (Words of a weight that rounds to nothing there are never drawn.)
+ *   logits       dev [N][ld] float or bfloat16
+ *   temperature  dev f32[N] or NULL: 1;  top_k dev i32[N] or NULL: all;  top_p dev f32[N] or NULL: 1;  min_p dev f32[N] or NULL: 0
+ *   u            dev f32[N]
+ *   word         dev i32[N] out;  logprob dev f32[N] out or NULL
+ * N = 0 is a no-op.  V <= 2^30.
+ */
+int rnnlm_sample(int N, int V, int dtype, const void *logits, long long ld, const float *temperature_or_null,
+                 const int32_t *top_k_or_null, const float *top_p_or_null, const float *min_p_or_null, const float *u,
+                 int32_t *word, float *logprob_or_null, void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* Bytes of workspace rnnlm_distill needs (0 for N <= 0 or V <= 0). */
+size_t rnnlm_distill_workspace_bytes(int N, int V);
+
+/*
+ * Loss of a student's rows of logits against a teacher's top K logits and, with weight a = label_weight, a label; and, when
+ * `grad` is given, its gradient in the same call.  Row n, T = temperature:
+ *   q = softmax(teacher_logit / T) over the K entries,  p = softmax(z / T),  p1 = softmax(z)  (both over all V words)
+ *   loss[n]    = (1 - a) T^2 sum_k q_k (log q_k - log p[word_k]) - a log p1[label]
+ *   grad[n][i] = row_weight[n] ((1 - a) T (p_i - sum of q_k with word_k = i) + a (p1_i - [i = label]))
+ *   logits         dev [N][ld] float or bfloat16
+ *   teacher_word   dev i32[N][K]  -1: no entry.  Repeated words add up.
+ *   teacher_logit  dev f32[N][K]  -infinity: an entry of probability 0
+ *   label          dev i32[N], -1: none; or NULL, with a = 0
+ *   temperature    > 0, finite;  label_weight in [0, 1]
+ *   row_weight     dev f32[N] or NULL: 1  (what the loss of a row weighs in the sum that is trained on)
+ *   loss           dev f32[N] out, without row_weight
+ *   stats          dev f32[N][4] out, for rnnlm_distill_backward: max z, 1 / sum exp((z - max) / T), 1 / sum exp(z - max), 0
+ *   grad           dev [N][grad_ld] of the logits' type, out, or NULL.  May be the logits themselves (same address and stride).
+ * A row without entries of its own (none, or all of probability 0) or with a = 1 has no soft part, one without a label or with
+ * a = 0 no hard part; with neither, loss and gradient are 0 whatever the logits.  Logits of -infinity have probability 0.  A
+ * teacher's word that the student cannot say makes the loss infinite.  Loss and gradient of a row are NaN where a word or label
+ * is outside [0, V) (and not -1), a teacher's logit is NaN or +infinity, or, in a row with a part, a logit is NaN or
+ * +infinity or none is finite.
+ * N = 0 is a no-op; K = 0 is labels only.  V <= 2^30.
+ */
+int rnnlm_distill(int N, int V, int K, int dtype, const void *logits, long long ld, const int32_t *teacher_word,
+                  const float *teacher_logit, const int32_t *label_or_null, float temperature, float label_weight,
+                  const float *row_weight_or_null, float *loss, float *stats, void *grad_or_null, long long grad_ld,
+                  void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* The gradient alone, from the statistics that rnnlm_distill left for the same logits and temperature (what a training program calls
+ * when the weight of a row's loss is known only later).  Arguments as above. */
+int rnnlm_distill_backward(int N, int V, int K, int dtype, const void *logits, long long ld, const int32_t *teacher_word,
+                           const float *teacher_logit, const int32_t *label_or_null, float temperature, float label_weight,
+                           const float *row_weight_or_null, const float *stats, void *grad, long long grad_ld, void *hip_stream);
 
 #ifdef __cplusplus
 }

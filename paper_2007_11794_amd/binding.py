@@ -28,7 +28,8 @@ EXPORTS = ["rnnlm_strerror", "rnnlm_load", "rnnlm_free", "rnnlm_model_share", "r
            "rnnlm_index_free", "rnnlm_index_reset", "rnnlm_index_intern", "rnnlm_index_fetch",
            "rnnlm_index_stats", "rnnlm_huffman_build", "rnnlm_hs_load", "rnnlm_hs_step", "rnnlm_hs_time_query",
            "rnnlm_probe_mfma_rate", "rnnlm_time_empty_launch", "rnnlm_outproj_kernel_name",
-           "rnnlm_one_launch"]
+           "rnnlm_one_launch", "rnnlm_q4_matvec", "rnnlm_q4_quantize", "rnnlm_sample_workspace_bytes", "rnnlm_sample",
+           "rnnlm_distill_workspace_bytes", "rnnlm_distill", "rnnlm_distill_backward"]
 
 
 class RnnlmError(RuntimeError):
@@ -114,6 +115,21 @@ def lib() -> ctypes.CDLL:
         L.rnnlm_index_fetch.restype = I
         L.rnnlm_index_stats.argtypes = [P, P, ctypes.POINTER(ctypes.c_int64)]
         L.rnnlm_index_stats.restype = I
+        LL, F = ctypes.c_longlong, ctypes.c_float
+        L.rnnlm_q4_matvec.argtypes = [I, I, I, I, P, LL, I, P, P, P, I, P, LL, I, P, LL, P]
+        L.rnnlm_q4_matvec.restype = I
+        L.rnnlm_q4_quantize.argtypes = [I, I, I, P, P, P, P]
+        L.rnnlm_q4_quantize.restype = I
+        L.rnnlm_sample_workspace_bytes.argtypes = [I, I]
+        L.rnnlm_sample_workspace_bytes.restype = Z
+        L.rnnlm_sample.argtypes = [I, I, I, P, LL, P, P, P, P, P, P, P, P, Z, P]
+        L.rnnlm_sample.restype = I
+        L.rnnlm_distill_workspace_bytes.argtypes = [I, I]
+        L.rnnlm_distill_workspace_bytes.restype = Z
+        L.rnnlm_distill.argtypes = [I, I, I, I, P, LL, P, P, P, F, F, P, P, P, P, LL, P, Z, P]
+        L.rnnlm_distill.restype = I
+        L.rnnlm_distill_backward.argtypes = [I, I, I, I, P, LL, P, P, P, F, F, P, P, P, LL, P]
+        L.rnnlm_distill_backward.restype = I
         _lib = L
     return _lib
 
@@ -510,3 +526,111 @@ def rnnlm_hs_time_query(model: RnnlmModel, query_word, h_out, logprob, repeats: 
                                      _dev(h_out, torch.float32, "h_out"), _dev(logprob, torch.float32, "logprob"),
                                      int(repeats), _stream(stream), ctypes.byref(ms)), "rnnlm_hs_time_query")
     return ms.value
+
+
+def _rows(t, name, dtype=None):
+    """(pointer, stride of a row, rnnlm_dtype) of a device matrix whose rows are contiguous, in float32 or bfloat16."""
+    import torch
+    code = RNNLM_F32 if t.dtype == torch.float32 else RNNLM_BF16 if t.dtype == torch.bfloat16 else None
+    if t.dim() != 2 or not t.is_cuda or code is None or (t.shape[1] > 1 and t.stride(1) != 1) or (dtype is not None and t.dtype != dtype):
+        raise TypeError("%s must be a device matrix of contiguous rows in %s" % (name, dtype or "float32 or bfloat16"))
+    return t.data_ptr() or None, int(t.stride(0)) if t.shape[0] > 1 else max(int(t.stride(0)), int(t.shape[1])), code
+
+
+def rnnlm_q4_matvec(codes, scales, group: int, x, y, zeros=None, bias=None, stream=None):
+    """y [B,V] = rows of x [B,H] times 4-bit weights: codes uint8 [V, at least ceil(H / 2)] (row stride free), scales float32 or
+    bfloat16 [ceil(H / group), V], zeros uint8 of the same shape or None (8 everywhere), bias float32 [V] or None."""
+    import torch
+    (B, H), V = x.shape, int(codes.shape[0])
+    if codes.dim() != 2 or not codes.is_cuda or codes.dtype != torch.uint8 or (codes.shape[1] > 1 and codes.stride(1) != 1):
+        raise TypeError("codes must be a device matrix of contiguous rows in torch.uint8")
+    if group not in (32, 64, 128):
+        raise ValueError("group must be 32, 64 or 128")
+    shape = (-(-H // group), V)
+    if y.shape != (B, V) or codes.shape[1] < -(-H // 2) or scales.shape != shape or (zeros is not None and zeros.shape != shape) or \
+            (bias is not None and bias.shape != (V,)):
+        raise TypeError("shape mismatch")
+    if scales.dtype not in (torch.float32, torch.bfloat16):
+        raise TypeError("scales must be float32 or bfloat16")
+    (px, ldx, tx), (py, ldy, ty) = _rows(x, "x"), _rows(y, "y")
+    code_ld = int(codes.stride(0)) if V > 1 else max(int(codes.stride(0)), int(codes.shape[1]))
+    _check(lib().rnnlm_q4_matvec(int(B), V, int(H), int(group), codes.data_ptr() or None, code_ld,
+                                 RNNLM_F32 if scales.dtype == torch.float32 else RNNLM_BF16, _dev(scales, scales.dtype, "scales"),
+                                 _dev(zeros, torch.uint8, "zeros"), _dev(bias, torch.float32, "bias"), tx, px, ldx, ty, py, ldy,
+                                 _stream(stream)), "rnnlm_q4_matvec")
+
+
+def rnnlm_q4_quantize(w: np.ndarray, group: int, zeros: bool = False):
+    """Host float32 weights [V,H] to (codes uint8 [V, ceil(H / 2)], scales float32 [ceil(H / group), V], zeros uint8 or None)."""
+    w = np.ascontiguousarray(w, dtype=np.float32)
+    if w.ndim != 2 or group not in (32, 64, 128):
+        raise TypeError("w must be a matrix, group 32, 64 or 128")
+    V, H = w.shape
+    codes = np.zeros((V, -(-H // 2)), dtype=np.uint8)
+    scale = np.zeros((-(-H // group), V), dtype=np.float32)
+    zero = np.zeros_like(scale, dtype=np.uint8) if zeros else None
+    _check(lib().rnnlm_q4_quantize(V, H, int(group), w.ctypes.data, codes.ctypes.data, scale.ctypes.data,
+                                   zero.ctypes.data if zeros else None), "rnnlm_q4_quantize")
+    return codes, scale, zero
+
+
+def rnnlm_sample_workspace_bytes(N: int, V: int) -> int:
+    return int(lib().rnnlm_sample_workspace_bytes(int(N), int(V)))
+
+
+def rnnlm_sample(logits, u, word, logprob, workspace, temperature=None, top_k=None, top_p=None, min_p=None, stream=None):
+    """A word from each row of logits [N,V] (float32 or bfloat16) by the uniform numbers u [N]; temperature, top_p, min_p float32
+    [N] or None, top_k int32 [N] or None; word int32 [N] out, logprob float32 [N] out or None; workspace uint8 device tensor of
+    rnnlm_sample_workspace_bytes(N, V)."""
+    import torch
+    N, V = logits.shape
+    if any(t is not None and t.shape != (N,) for t in (u, word, logprob, temperature, top_k, top_p, min_p)):
+        raise TypeError("shape mismatch")
+    p, ld, code = _rows(logits, "logits")
+    _check(lib().rnnlm_sample(int(N), int(V), code, p, ld, _dev(temperature, torch.float32, "temperature"),
+                              _dev(top_k, torch.int32, "top_k"), _dev(top_p, torch.float32, "top_p"),
+                              _dev(min_p, torch.float32, "min_p"), _dev(u, torch.float32, "u"), _dev(word, torch.int32, "word"),
+                              _dev(logprob, torch.float32, "logprob"), _dev(workspace, torch.uint8, "workspace"),
+                              0 if workspace is None else workspace.numel(), _stream(stream)), "rnnlm_sample")
+
+
+def rnnlm_distill_workspace_bytes(N: int, V: int) -> int:
+    return int(lib().rnnlm_distill_workspace_bytes(int(N), int(V)))
+
+
+def _distill_args(logits, teacher_word, teacher_logit, labels, row_weight, stats, grad):
+    import torch
+    N, V = logits.shape
+    K = int(teacher_word.shape[1]) if teacher_word.dim() == 2 else 0
+    if teacher_word.shape != (N, K) or teacher_logit.shape != (N, K) or stats.shape != (N, 4) or \
+            (labels is not None and labels.shape != (N,)) or (row_weight is not None and row_weight.shape != (N,)) or \
+            (grad is not None and grad.shape != (N, V)):
+        raise TypeError("shape mismatch")
+    p, ld, code = _rows(logits, "logits")
+    pg, ldg, _ = (None, 0, 0) if grad is None else _rows(grad, "grad", logits.dtype)
+    return (int(N), int(V), K, code, p, ld, _dev(teacher_word, torch.int32, "teacher_word"),
+            _dev(teacher_logit, torch.float32, "teacher_logit"), _dev(labels, torch.int32, "labels")), (pg, ldg)
+
+
+def rnnlm_distill(logits, teacher_word, teacher_logit, loss, stats, workspace, temperature: float = 1.0, labels=None,
+                  label_weight: float = 0.0, row_weight=None, grad=None, stream=None):
+    """Loss [N] of logits [N,V] (float32 or bfloat16) against teacher_word int32 / teacher_logit float32 [N,K] and labels int32 [N] or
+    None; stats float32 [N,4] out; grad [N,V] of the logits' type out, or None; row_weight float32 [N] or None: what the loss of each
+    row weighs in the gradient; workspace uint8 device tensor of rnnlm_distill_workspace_bytes(N, V)."""
+    import torch
+    a, (pg, ldg) = _distill_args(logits, teacher_word, teacher_logit, labels, row_weight, stats, grad)
+    if loss.shape != (a[0],):
+        raise TypeError("shape mismatch")
+    _check(lib().rnnlm_distill(*a, float(temperature), float(label_weight), _dev(row_weight, torch.float32, "row_weight"),
+                               _dev(loss, torch.float32, "loss"), _dev(stats, torch.float32, "stats"), pg, ldg,
+                               _dev(workspace, torch.uint8, "workspace"), 0 if workspace is None else workspace.numel(),
+                               _stream(stream)), "rnnlm_distill")
+
+
+def rnnlm_distill_backward(logits, teacher_word, teacher_logit, stats, grad, temperature: float = 1.0, labels=None,
+                           label_weight: float = 0.0, row_weight=None, stream=None):
+    """The gradient of rnnlm_distill's loss from the stats it left."""
+    import torch
+    a, (pg, ldg) = _distill_args(logits, teacher_word, teacher_logit, labels, row_weight, stats, grad)
+    _check(lib().rnnlm_distill_backward(*a, float(temperature), float(label_weight), _dev(row_weight, torch.float32, "row_weight"),
+                                        _dev(stats, torch.float32, "stats"), pg, ldg, _stream(stream)), "rnnlm_distill_backward")

@@ -1,0 +1,226 @@
+"""The draw of a word against the definition in 64 bits: every limit and their combinations, ties, masks, the edges of a row."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2007_11794_amd as rn
+from ops_reference import sample_row
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+INF, NAN = float("inf"), float("nan")
+
+
+def dev(x, dtype):
+    return None if x is None else torch.as_tensor(np.asarray(x), dtype=dtype).to(DEV)
+
+
+def draw(z, u, T=None, k=None, p=None, m=None, logprob=True, workspace=None):
+    """z: device matrix."""
+    N, V = z.shape
+    word = torch.full((N,), -7, dtype=torch.int32, device=DEV)
+    lp = torch.full((N,), 7.0, device=DEV) if logprob else None
+    ws = torch.randint(0, 256, (rn.rnnlm_sample_workspace_bytes(N, V),), dtype=torch.uint8, device=DEV) if workspace is None else workspace
+    f = torch.float32
+    rn.rnnlm_sample(z, dev(u, f), word, lp, ws, temperature=dev(T, f), top_k=dev(k, torch.int32), top_p=dev(p, f), min_p=dev(m, f))
+    torch.cuda.synchronize()
+    return word.cpu().numpy(), None if lp is None else lp.cpu().numpy()
+
+
+def check(z, u, T=None, k=None, p=None, m=None):
+    word, lp = draw(z, u, T, k, p, m)
+    rows, V = z.double().cpu().numpy(), z.shape[1]
+    one = 2.0 ** -(62 - int(np.ceil(np.log2(V))) if V > 1 else -62)
+    at = lambda x, n, other: other if x is None else np.float64(np.asarray(x, np.float32)[n])  # noqa: E731
+    for n in range(len(rows)):
+        want, want_lp, w = sample_row(rows[n], at(u, n, 0.0), at(T, n, 1.0), 0 if k is None else int(k[n]), at(p, n, 1.0), at(m, n, 0.0))
+        assert word[n] == want, (n, word[n], want)
+        if want < 0:
+            assert np.isnan(lp[n])
+        else:     # rounded once to 32 bits; the word's weight is good to half a unit of the fixed-point number, the sum to better than that
+            assert abs(lp[n] - want_lp) <= 2 ** -23 * abs(want_lp) + 2 * one / w + 1e-12, (n, lp[n], want_lp)
+
+
+def logits(N, V, seed, dtype=torch.float32, spread=2.0, mask=0.02):
+    rng = np.random.default_rng(seed)
+    z = rng.standard_normal((N, V)) * spread - 1.1 * np.log(np.arange(1, V + 1))
+    z[rng.random((N, V)) < mask] = -np.inf
+    z[:, rng.integers(0, V)] = 0.0                                 # something is left
+    return torch.from_numpy(z.astype(np.float32)).to(DEV).to(dtype)
+
+
+def limits(N, V, seed):
+    rng = np.random.default_rng(seed)
+    T = np.where(rng.random(N) < 0.1, 0.0, rng.uniform(0.3, 2.0, N))
+    k = np.where(rng.random(N) < 0.5, 0, np.exp(rng.uniform(0, np.log(1.2 * V + 1), N)).astype(int))
+    p = np.where(rng.random(N) < 0.4, 1.0, rng.uniform(0.02, 0.999, N))
+    m = np.where(rng.random(N) < 0.6, 0.0, rng.uniform(0.0, 0.3, N))
+    return rng.random(N).astype(np.float32) * np.float32(0.99999), T, k, p, m
+
+
+VOCABULARIES = [1, 2, 3, 63, 64, 65, 255, 1000, 1023, 1025, 4096, 4099, 8193, 20011, 65536, 65537, 131073, 200003]
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("V", VOCABULARIES)
+def test_all_limits(V, dtype):
+    for N in (1, 3, 40) if V < 100000 else (1, 5):
+        u, T, k, p, m = limits(N, V, V + N)
+        check(logits(N, V, V * 3 + N, dtype), u, T, k, p, m)
+
+
+@pytest.mark.parametrize("rule", ["none", "k", "p", "m", "T"])
+@pytest.mark.parametrize("N,V", [(2, 300), (300, 1500), (2, 70001), (17, 40000)])
+def test_one_limit_at_a_time(rule, N, V):
+    u, T, k, p, m = limits(N, V, 11)
+    check(logits(N, V, 12), u, T=T if rule == "T" else None, k=k if rule == "k" else None, p=p if rule == "p" else None, m=m if rule == "m" else None)
+
+
+@pytest.mark.parametrize("V", [50, 5000, 100000])
+def test_many_rows(V):
+    N = 600 if V < 100000 else 270
+    u, T, k, p, m = limits(N, V, 5)
+    check(logits(N, V, 6, torch.bfloat16), u, T, k, p, m)
+
+
+@pytest.mark.parametrize("V", [7, 700, 33000, 140000])
+def test_rows_of_few_values(V):
+    """Hundreds of words of one logit at every border."""
+    N = 24
+    rng = np.random.default_rng(V)
+    z = torch.from_numpy(rng.integers(-3, 3, (N, V)).astype(np.float32)).to(DEV)
+    u, T, k, p, m = limits(N, V, 9)
+    check(z, u, T, k, p, m)
+    flat = torch.zeros((N, V), device=DEV)
+    flat[:, ::3] = -0.0                                            # the same number as 0
+    check(flat, u, T, k, p, m)
+
+
+def test_near_ties():
+    """Neighbouring floats: the order goes by all bits of the logits, however little their weights differ."""
+    V = 3000
+    z = (torch.arange(V, dtype=torch.int32) * 7919 % V + 0x3F800000).view(torch.float32)[None].repeat(8, 1).to(DEV)
+    check(z, np.linspace(0, 0.99, 8), k=[1, 2, 10, 100, 1000, 2999, 3000, 3001])
+    check(z, np.linspace(0, 0.99, 8), p=[0.001, 0.01, 0.1, 0.3, 0.5, 0.9, 0.99, 0.9999])
+
+
+def test_infinities_masks_and_rows_without_a_word():
+    V = 5000
+    for dtype in (torch.float32, torch.bfloat16):
+        low = torch.finfo(dtype).min
+        z = logits(12, V, 2, dtype)
+        z[1] = -INF
+        z[2, 77] = NAN
+        z[3, [5, 900, 4999]] = INF
+        z[4] = low                                                 # all masked with the lowest number: all alike
+        z[5] = low
+        z[5, 123] = -50.0
+        z[6] = -INF
+        z[6, V - 1] = low
+        z[7, :] = INF
+        z[8, 4] = torch.finfo(dtype).max
+        u, T, k, p, m = limits(12, V, 3)
+        check(z, u)
+        check(z, u, T, k, p, m)
+        check(z, u, T=np.full(12, 1e-30), p=p)
+        check(z, u, T=np.full(12, 1e30), k=k)
+
+
+def test_bad_limits():
+    z = logits(12, 100, 4)
+    ok = np.full(12, 0.5)
+    for name, values in (("T", [-1.0, NAN, INF, 1e-45, 3e38]), ("p", [NAN, -1.0, 0.0, 1e-30, 2.0, INF]), ("m", [NAN, -1.0, 0.0, 1.0, 3.0, INF]), ("u", [-0.1, 1.0, NAN, 0.0, 0.99999994, INF])):
+        a = {"u": ok, "T": None, "k": None, "p": None, "m": None}
+        a[name] = np.resize(values, 12)
+        check(z, **a)
+    check(z, ok, k=[-5, 0, 1, 99, 100, 101, 2 ** 31 - 1, -2 ** 31, 3, 3, 3, 3])
+
+
+def test_edges_of_u():
+    """The first and the last word that can come."""
+    V = 2049
+    z = torch.full((4, V), -INF, device=DEV)
+    z[:, 700:1500] = 0.0
+    word, _ = draw(z, [0.0, 0.99999994, 0.5, 0.25])
+    assert list(word) == [700, 1499, 1100, 900]
+
+
+def test_strides_and_alignment():
+    for dtype in (torch.float32, torch.bfloat16):
+        wide = torch.full((6, 3100), 50.0, device=DEV, dtype=dtype)
+        for off in (0, 1, 2, 3, 5):
+            for V in (1, 8, 2999):
+                z = wide[:, off:off + V]
+                z.copy_(logits(6, V, off, dtype))
+                u, T, k, p, m = limits(6, V, off)
+                check(z, u, T, k, p, m)
+                z.fill_(50.0)
+
+
+def test_rows_beyond_two_gigabytes():
+    V, ld = 1500, 1 << 30
+    big = torch.empty(2 * ld + V, dtype=torch.float32, device=DEV)
+    z = torch.as_strided(big, (3, V), (ld, 1))
+    z.copy_(logits(3, V, 8))
+    check(z, [0.2, 0.5, 0.8], k=[0, 5, 50], p=[0.9, 0.8, 1.0])
+
+
+def test_the_word_does_not_depend_on_the_batch_and_repeats():
+    V = 90001
+    z = logits(40, V, 10)
+    u, T, k, p, m = limits(40, V, 11)
+    first = draw(z, u, T, k, p, m)
+    again = draw(z, u, T, k, p, m)
+    assert np.array_equal(first[0], again[0]) and np.array_equal(first[1], again[1])
+    for n in (0, 13, 39):
+        s = slice(n, n + 1)
+        one = draw(z[s], u[s], T[s], k[s], p[s], m[s])
+        assert one[0][0] == first[0][n] and one[1][0] == first[1][n]
+
+
+def test_frequencies():
+    """Drawn by evenly spaced numbers, words come as often as their share says, to one draw."""
+    N, V = 4000, 40
+    z = torch.randn((1, V), device=DEV).expand(N, V).contiguous()
+    word, _ = draw(z, (np.arange(N) + 0.5) / N, T=np.full(N, 0.8))
+    share = torch.softmax(z[0].double() / np.float32(0.8).astype(np.float64), 0).cpu().numpy()
+    assert (np.abs(np.bincount(word, minlength=V) - N * share) <= 1.001).all()
+
+
+def test_without_logprob_without_rows_and_a_workspace_kept():
+    z = logits(3, 500, 1)
+    assert draw(z, [0.1, 0.5, 0.9], logprob=False)[1] is None
+    rn.rnnlm_sample(z[:0], torch.empty(0, device=DEV), torch.empty(0, dtype=torch.int32, device=DEV), None, None)
+    ws = torch.empty(rn.rnnlm_sample_workspace_bytes(40, 70000), dtype=torch.uint8, device=DEV)
+    for N, V in ((40, 70000), (1, 100), (2, 70000), (40, 70000)):       # a larger workspace serves, whatever the last call left in it
+        z = logits(N, V, 3)
+        u, T, k, p, m = limits(N, V, 4)
+        a, b = draw(z, u, T, k, p, m), draw(z, u, T, k, p, m, workspace=ws)
+        assert np.array_equal(a[0], b[0]) and np.array_equal(a[1], b[1])
+
+
+@pytest.mark.parametrize("N,V", [(2, 60000), (30, 3000)])
+def test_another_stream_and_a_graph(N, V):
+    zs = [logits(N, V, s) for s in range(3)]
+    u, T, k, p, m = limits(N, V, 1)
+    want = [draw(z, u, T, k, p, m) for z in zs]
+    f = torch.float32
+    a = dict(temperature=dev(T, f), top_k=dev(k, torch.int32), top_p=dev(p, f), min_p=dev(m, f))
+    ud, buf, word, lp = dev(u, f), zs[0].clone(), torch.empty(N, dtype=torch.int32, device=DEV), torch.empty(N, device=DEV)
+    ws = torch.empty(rn.rnnlm_sample_workspace_bytes(N, V), dtype=torch.uint8, device=DEV)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        rn.rnnlm_sample(buf, ud, word, lp, ws, **a)
+    side.synchronize()
+    assert np.array_equal(word.cpu().numpy(), want[0][0])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        rn.rnnlm_sample(buf, ud, word, lp, ws, **a)
+    for i in (1, 2, 0, 1):
+        buf.copy_(zs[i])
+        word.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert np.array_equal(word.cpu().numpy(), want[i][0]) and np.array_equal(lp.cpu().numpy(), want[i][1])
+        assert np.array_equal(draw(zs[2], u, T, k, p, m)[0], want[2][0])
