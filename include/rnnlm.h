@@ -456,8 +456,9 @@ size_t rnnlm_distill_workspace_bytes(int N, int V);
  * teacher's word that the student cannot say makes the loss infinite.  Loss and gradient of a row are NaN where a word or label
  * is outside [0, V) (and not -1), a teacher's logit is NaN or +infinity, or, in a row with a part, a logit is NaN or
  * +infinity or none is finite.
- * N = 0 is a no-op; K = 0 is labels only.  V <= 2^30.
+ * N = 0 is a no-op; K = 0 is labels only.  V <= 2^30, K <= RNNLM_DISTILL_MAX_K (RNNLM_ERANGE).
  */
+#define RNNLM_DISTILL_MAX_K 4096
 int rnnlm_distill(int N, int V, int K, int dtype, const void *logits, long long ld, const int32_t *teacher_word,
                   const float *teacher_logit, const int32_t *label_or_null, float temperature, float label_weight,
                   const float *row_weight_or_null, float *loss, float *stats, void *grad_or_null, long long grad_ld,

@@ -47,7 +47,7 @@ bool aligned(const void *p, size_t to) { return reinterpret_cast<uintptr_t>(p) %
 int check_distill(int N, int V, int K, int dtype, const void *logits, long long ld, const int32_t *teacher_word, const float *teacher_logit,
                   const int32_t *label, float T, float a, const void *grad, long long grad_ld) {
     if (N < 0 || V <= 0 || K < 0 || !known_dtype(dtype)) return RNNLM_EINVAL;
-    if (V > kMaxWords || N > kMaxRows || K > kMaxRows) return RNNLM_ERANGE;
+    if (V > kMaxWords || N > kMaxRows || K > RNNLM_DISTILL_MAX_K) return RNNLM_ERANGE;
     if (ld < V || ld > kMaxStride || (grad && (grad_ld < V || grad_ld > kMaxStride))) return RNNLM_EINVAL;
     if (!(T > 0.f) || !std::isfinite(T) || !(a >= 0.f && a <= 1.f) || (!label && a != 0.f)) return RNNLM_EINVAL;
     if (N == 0) return RNNLM_OK;

@@ -1,4 +1,9 @@
 // Loss of rows of logits against a teacher's top logits and labels, and its gradient.
+//
+// A row is read once: it stays in the registers of its workgroup from its maximum over its sums to its gradient (what does not fit, of
+// rows beyond kRegs vectors a thread, is read again).  The teacher's words are some tens among tens of thousands: the gradient is
+// written as if there were none, and their own places once more behind it, from the logits gathered before.  Where rows are too few
+// to fill the chip they are cut into segments: one launch for a segment's maximum and sums, one that joins them and goes on.
 #include "device_utils.h"
 #include "ops.h"
 
@@ -6,11 +11,6 @@ namespace rnnlm {
 
 namespace {
 
-constexpr int kThreads = 256, kWaves = kThreads / 64;
-
-__device__ __forceinline__ float logit(const void *p, long long i, bool bf16) {
-    return bf16 ? bf16_to_f32(static_cast<const uint16_t *>(p)[i]) : static_cast<const float *>(p)[i];
-}
 // e^(x / T), per = log2(e) / T in two floats: what rounding the exponent's argument loses goes into a first-order term, so that shares
 // of any size are good to some 2^-22 of themselves.
 struct Exponent {
@@ -25,123 +25,594 @@ struct Exponent {
         return y > -INFINITY ? fast_exp2(y) * (1.f + kLn2 * (__builtin_fmaf(x, per, -y) + x * rest)) : 0.f;
     }
 };
-__device__ __forceinline__ float block_sum(float v, float *part) {
-    v = wave_sum(v);
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
-    __syncthreads();
-    v = 0.f;
-    for (int w = 0; w < kWaves; ++w) v += part[w];
-    return v;
+
+typedef u32x4 u32x4_any __attribute__((aligned(2)));         // rows may start at any element
+
+// Vectors of 16 bytes of a row.
+template <typename Z> struct Row;
+template <> struct Row<float> {
+    static constexpr int E = 4;
+    static __device__ __forceinline__ float get(u32x4 v, int i) { return __uint_as_float(v[i]); }
+    static __device__ __forceinline__ u32x4 make(const float (&x)[4]) { return u32x4{__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3])}; }
+    static __device__ __forceinline__ float one(const float *p) { return *p; }
+    static __device__ __forceinline__ void put(float *p, float x) { *p = x; }
+    static __device__ __forceinline__ u32x4 nothing() { return u32x4{0xFF800000u, 0xFF800000u, 0xFF800000u, 0xFF800000u}; }
+};
+template <> struct Row<uint16_t> {
+    static constexpr int E = 8;
+    static __device__ __forceinline__ float get(u32x4 v, int i) { return __uint_as_float(i & 1 ? v[i >> 1] & 0xFFFF0000u : v[i >> 1] << 16); }
+    static __device__ __forceinline__ u32x4 make(const float (&x)[8]) { return u32x4{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7])}; }
+    static __device__ __forceinline__ float one(const uint16_t *p) { return bf16_to_f32(*p); }
+    static __device__ __forceinline__ void put(uint16_t *p, float x) { *p = (uint16_t)pack_bf16x2(x, 0.f); }
+    static __device__ __forceinline__ u32x4 nothing() { return u32x4{0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u}; }
+};
+
+// The compiler takes this for another value: what it computed from the old one is not kept in registers for later (a row's differences
+// from its maximum, twice the registers of a row in bfloat16, went to scratch memory).
+__device__ __forceinline__ void forget(u32x4 &v) { asm volatile("" : "+v"(v)); }
+__device__ __forceinline__ int forget(int v) { asm volatile("" : "+v"(v)); return v; }
+
+// Vector `i` of a row, or of a segment: p is the same in all lanes and i * 16 fits 32 bits (a row has at most 2^30 elements of 4 bytes),
+// so that the address is one register.  Elements behind the last whole vector, fewer than E, are one for each of the first threads.
+template <typename Z>
+__device__ __forceinline__ u32x4 load_vector(const Z *p, int i) {
+    return *reinterpret_cast<const u32x4_any *>(reinterpret_cast<const char *>(p) + (uint32_t)i * 16u);
 }
-__device__ __forceinline__ float block_max(float v, float *part) {
-    v = wave_max(v);
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
-    __syncthreads();
-    v = -INFINITY;
-    for (int w = 0; w < kWaves; ++w) v = fmaxf(v, part[w]);
-    return v;
+template <typename Z>
+__device__ __forceinline__ void store_vector(Z *p, int i, const float (&x)[Row<Z>::E]) {
+    *reinterpret_cast<u32x4_any *>(reinterpret_cast<char *>(p) + (uint32_t)i * 16u) = Row<Z>::make(x);
+}
+template <typename Z>
+__device__ __forceinline__ float load_tail(const Z *p, int n) {
+    const int at = n / Row<Z>::E * Row<Z>::E + (int)threadIdx.x;
+    return threadIdx.x < (unsigned)Row<Z>::E && at < n ? Row<Z>::one(p + at) : -INFINITY;
+}
+template <typename Z>
+__device__ __forceinline__ void store_tail(Z *p, int n, float x) {
+    const int at = n / Row<Z>::E * Row<Z>::E + (int)threadIdx.x;
+    if (threadIdx.x < (unsigned)Row<Z>::E && at < n) Row<Z>::put(p + at, x);
 }
 
-// The plain form: a workgroup per row, three passes over it.
-__global__ __launch_bounds__(kThreads) void distill_plain_kernel(DistillArgs a, bool forward) {
-    __shared__ float part[kWaves];
-    const int tid = threadIdx.x;
-    for (int n = blockIdx.x; n < a.N; n += gridDim.x) {
-        const long long base = n * a.ld;
-        const int32_t *tw = a.teacher_word + (long long)n * a.K;
-        const float *tl = a.teacher_logit + (long long)n * a.K;
-        const Exponent exponent(a.T);
-        const float per = exponent.per;
-        const int label = a.label ? a.label[n] : -1;
-        // teacher
-        float t_top = -INFINITY;
-        bool bad = label < -1 || label >= a.V;
-        for (int k = tid; k < a.K; k += kThreads) {
+// Sums (or maxima) of M values over the workgroup, in a fixed order; `part` is LDS scratch of M * waves floats, free again on return.
+template <int M, bool MAX, int WAVES>
+__device__ __forceinline__ void block_reduce(float (&v)[M], float *part) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+    for (int i = 0; i < M; ++i) v[i] = MAX ? wave_max(v[i]) : wave_sum(v[i]);
+    if (lane == 0)
+#pragma unroll
+        for (int i = 0; i < M; ++i) part[i * WAVES + wave] = v[i];
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < M; ++i) {
+        float r = lane < WAVES ? part[i * WAVES + lane] : MAX ? -INFINITY : 0.f;
+        v[i] = MAX ? wave_max(r) : wave_sum(r);
+    }
+    __syncthreads();
+}
+
+// The teacher's list of one row, in LDS.
+struct List {
+    int K;
+    int *word;           // [K], -1: none
+    float *q, *z;        // [K] the teacher's logit, then its share; the student's logit
+    int *hash;           // [hash_mask + 1]
+    int hash_mask;
+    __device__ List(char *lds, int K, int hash_size) : K(K), hash_mask(hash_size - 1) {
+        word = reinterpret_cast<int *>(lds);
+        q = reinterpret_cast<float *>(word + K);
+        z = q + K;
+        hash = reinterpret_cast<int *>(z + K);
+    }
+    // Words and logits from memory; returns this thread's largest logit, +infinity where something is wrong with an entry.
+    template <int THREADS>
+    __device__ __forceinline__ float read(const DistillArgs &a, int n) {
+        const int32_t *tw = a.teacher_word + (long long)n * K;
+        const float *tl = a.teacher_logit + (long long)n * K;
+        float top = -INFINITY;
+        for (int i = threadIdx.x; i <= hash_mask; i += THREADS) hash[i] = -1;
+        for (int k = threadIdx.x; k < K; k += THREADS) {
+            const int w = tw[k];
             const float t = tl[k];
-            if (tw[k] == -1) continue;
-            bad |= tw[k] < -1 || tw[k] >= a.V || t != t || t == INFINITY;
-            t_top = fmaxf(t_top, t);
+            word[k] = w;
+            q[k] = t;
+            if (w != -1) top = fmaxf(top, w < -1 || w >= a.V || t != t ? INFINITY : t);
         }
-        t_top = block_max(t_top, part);
-        bad = __syncthreads_or(bad);
-        const bool soft = t_top > -INFINITY, hard = label >= 0;
-        float t_sum = 0.f;
-        if (soft)
-            for (int k = tid; k < a.K; k += kThreads)
-                if (tw[k] >= 0) t_sum += exponent.fine(tl[k] - t_top);
-        t_sum = block_sum(t_sum, part);
-        const float lq = logf(t_sum);
-        float top, inv_T, inv_1;
-        if (forward) {
-            top = -INFINITY;
-            bool nan = false;
-            for (int i = tid; i < a.V; i += kThreads) {
-                const float z = logit(a.logits, base + i, a.bf16);
-                nan |= z != z;
-                top = fmaxf(top, z);
+        return top;
+    }
+    // Puts this thread's words into the table; true where one is there already.
+    template <int THREADS>
+    __device__ __forceinline__ bool repeated() {
+        bool again = false;
+        for (int k = threadIdx.x; k < K; k += THREADS) {
+            const int w = word[k];
+            if (w < 0) continue;
+            for (uint32_t at = ((uint32_t)w * 0x9E3779B1u >> 7) & hash_mask;; at = (at + 1) & hash_mask) {     // (half of it stays free)
+                const int was = atomicCAS(&hash[at], -1, w);
+                if (was == -1) break;
+                if (was == w) { again = true; break; }
             }
-            top = block_max(top, part);
-            if (__syncthreads_or(nan)) top = quiet_nan();
-            float s_T = 0.f, s_1 = 0.f;
-            for (int i = tid; i < a.V; i += kThreads) {
-                const float d = logit(a.logits, base + i, a.bf16) - top;
-                s_T += fast_exp2(d * per);
-                s_1 += fast_exp2(d * kLog2e);
-            }
-            s_T = block_sum(s_T, part);
-            s_1 = block_sum(s_1, part);
-            const bool dead = !(s_T > 0.f) || top == INFINITY;               // NaN in it, or nothing finite
-            inv_T = dead ? quiet_nan() : 1.f / s_T;
-            inv_1 = dead ? quiet_nan() : 1.f / s_1;
-            float l = 0.f;
-            if (!bad && soft)
-                for (int k = tid; k < a.K; k += kThreads)
-                    if (tw[k] >= 0) {
-                        const float log_q = (tl[k] - t_top) / a.T - lq, q = exponent.fine(tl[k] - t_top) / t_sum;
-                        if (q > 0.f) l += q * (log_q - (logit(a.logits, base + tw[k], a.bf16) - top) / a.T + logf(s_T));
-                    }
-            l = soft && a.a < 1.f ? block_sum(l, part) * (1.f - a.a) * a.T * a.T : 0.f;
-            const bool hard_part = hard && a.a > 0.f, soft_part = soft && a.a < 1.f;
-            if (!bad && hard_part) l += a.a * (logf(s_1) - (logit(a.logits, base + label, a.bf16) - top));
-            if (bad || ((soft_part || hard_part) && dead)) l = quiet_nan();
-            if (tid == 0) {
-                a.loss[n] = l;
-                a.stats[4 * n] = top; a.stats[4 * n + 1] = inv_T; a.stats[4 * n + 2] = inv_1; a.stats[4 * n + 3] = 0.f;
-            }
-        } else {
-            top = a.stats[4 * n]; inv_T = a.stats[4 * n + 1]; inv_1 = a.stats[4 * n + 2];
         }
-        if (!a.grad) continue;
-        const float g = a.row_weight ? a.row_weight[n] : 1.f;
-        const float c_T = soft && a.a < 1.f ? g * (1.f - a.a) * a.T : 0.f, c_1 = hard && a.a > 0.f ? g * a.a : 0.f;
-        for (int i = tid; i < a.V; i += kThreads) {
-            const float d = logit(a.logits, base + i, a.bf16) - top;
-            float r = bad || ((c_T != 0.f || c_1 != 0.f) && inv_T != inv_T) ? quiet_nan() : 0.f;
-            if (c_T != 0.f) r += c_T * fast_exp2(d * per) * inv_T;
-            if (c_1 != 0.f) r += c_1 * fast_exp2(d * kLog2e) * inv_1;
-            if (c_T != 0.f)
-                for (int k = 0; k < a.K; ++k)
-                    if (tw[k] == i) r -= c_T * exponent.fine(tl[k] - t_top) / t_sum;
-            if (i == label) r -= c_1;
-            if (a.bf16) static_cast<uint16_t *>(a.grad)[n * a.grad_ld + i] = (uint16_t)pack_bf16x2(r, 0.f);
-            else static_cast<float *>(a.grad)[n * a.grad_ld + i] = r;
+        return again;
+    }
+    // What the teacher gives to the word of entry k: its share, or where words repeat the sum of theirs, in the order of the list, at the
+    // first of them; nothing (-1) at the others.
+    __device__ __forceinline__ float share_of(int k, bool repeats) const {
+        if (!repeats) return q[k];
+        float sum = 0.f;
+        for (int j = 0; j < K; ++j)
+            if (word[j] == word[k]) {
+                if (j < k) return -1.f;
+                sum += q[j];
+            }
+        return sum;
+    }
+};
+
+// The gradient of a row but for the teacher's words and the label.  TWO: shares at both temperatures, else those at one (`per`).
+template <bool TWO>
+struct RowGrad {
+    float top, per, c, c_1;        // weights times 1 / sums
+    bool dead;
+    __device__ RowGrad(const DistillArgs &a, float per_T, float top, float inv_T, float inv_1, float k_T, float k_1, bool bad) : top(top), per(per_T) {
+        dead = bad || ((k_T != 0.f || k_1 != 0.f) && inv_T != inv_T);
+        c = dead ? quiet_nan() : k_T != 0.f ? k_T * inv_T : 0.f;
+        c_1 = !dead && k_1 != 0.f ? k_1 * inv_1 : 0.f;
+        if (!TWO && c_1 != 0.f) { c = k_T != 0.f ? c + c_1 : c_1; per = kLog2e; }      // (both only at T = 1)
+    }
+    __device__ __forceinline__ bool nothing() const { return c == 0.f && c_1 == 0.f; }
+    __device__ __forceinline__ float operator()(float z) const {
+        const float d = z - top;
+        const float r = c * fast_exp2(d * per);
+        return TWO ? __builtin_fmaf(c_1, fast_exp2(d * kLog2e), r) : r;
+    }
+};
+
+// The places of the teacher's words and of the label within [from, from + len) of the row, written over what is there.  `in_list`: the label
+// is one of the words.  Called behind a barrier that awaited the stores.
+template <typename Z, int THREADS, typename Grad>
+__device__ __forceinline__ void write_listed(const DistillArgs &a, const List &list, const Grad &grad, Z *out, int from, int len, float k_T, float k_1, bool repeats,
+                                             int label, float z_label) {
+    bool mine = false;
+    for (int k = threadIdx.x; k_T != 0.f && k < list.K; k += THREADS) {
+        const int w = list.word[k];
+        if (w < from || w >= from + len) continue;
+        mine |= w == label;
+        const float q = list.share_of(k, repeats);
+        if (q >= 0.f) Row<Z>::put(out + w, grad(list.z[k]) - k_T * q - (w == label ? k_1 : 0.f));
+    }
+    const bool in_list = __syncthreads_or(mine);
+    if (threadIdx.x == 0 && !in_list && label >= from && label < from + len && k_1 != 0.f) Row<Z>::put(out + label, grad(z_label) - k_1);
+}
+
+// loss of a row: soft = sum q (log q - log p), the label's -log p
+__device__ __forceinline__ float row_loss(const DistillArgs &a, bool bad, bool soft_part, bool hard_part, bool dead, float soft, float hard) {
+    if (bad || ((soft_part || hard_part) && dead)) return quiet_nan();
+    float l = 0.f;
+    if (soft_part) l = (1.f - a.a) * a.T * a.T * soft;
+    if (hard_part) l += a.a * hard;
+    return l;
+}
+
+// Which exponentials a row takes.
+enum Form {
+    kOne,          // T = 1: the same for both parts
+    kTwoSums,      // T != 1: sums at both temperatures for the statistics, a gradient at one (label_weight 0 or 1)
+    kTwo           // T != 1, both parts
+};
+
+// One workgroup per row.
+template <typename Z, int THREADS, int R, int STASH, bool GRAD, Form FORM>
+__global__ __launch_bounds__(THREADS, 4) void distill_row_kernel(DistillArgs a, int hash_size) {
+    constexpr int E = Row<Z>::E, WAVES = THREADS / 64;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    __shared__ float part[3 * WAVES];
+    const int tid = threadIdx.x, n = blockIdx.x, V = a.V, vectors = V / E;
+    const Z *row = static_cast<const Z *>(a.logits) + n * a.ld;
+    const Exponent exponent(a.T);
+    const float per = exponent.per;
+    u32x4 *const stash = reinterpret_cast<u32x4 *>(lds);
+    List list(lds + STASH * THREADS * 16, a.K, hash_size);
+    const int label = a.label ? a.label[n] : -1;
+    const float t_mine = list.read<THREADS>(a, n);
+    // what stays in registers: vectors tid, tid + THREADS, ...
+    u32x4 v[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        v[r] = Row<Z>::nothing();
+        if (r * THREADS + tid < vectors) v[r] = load_vector(row, r * THREADS + tid);
+    }
+    const float z_tail = load_tail(row, V);
+    // This thread's maximum and its sums relative to it, so that exponentials are taken while other waves' vectors are on their way and
+    // not behind the whole row's maximum.
+    float mine = z_tail;
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int j = 0; j < E; ++j) mine = fmaxf(mine, Row<Z>::get(v[r], j));
+    float from = mine == -INFINITY ? 0.f : mine;
+    float at_T[E] = {}, at_1[E] = {};
+    auto add = [&](u32x4 x) {
+#pragma unroll
+        for (int j = 0; j < E; ++j) {
+            const float d = Row<Z>::get(x, j) - from;
+            at_T[j] += fast_exp2(d * per);
+            if (FORM != kOne) at_1[j] += fast_exp2(d * kLog2e);
+        }
+    };
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        forget(v[r]);
+        add(v[r]);
+    }
+    at_T[0] += fast_exp2((z_tail - from) * per);
+    if (FORM != kOne) at_1[0] += fast_exp2((z_tail - from) * kLog2e);
+    // What does not stay in registers, four vectors on their way at a time.  The first STASH of a thread stay in LDS.
+    for (int f = 0; R * THREADS + f * THREADS < vectors; f += 4) {
+        u32x4 x[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const int i = (R + f + q) * THREADS + tid;
+            x[q] = Row<Z>::nothing();
+            if (i < vectors) x[q] = load_vector(row, i);
+        }
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            if (GRAD && f + q < STASH) stash[(f + q) * THREADS + tid] = x[q];
+            float high = mine;
+#pragma unroll
+            for (int j = 0; j < E; ++j) high = fmaxf(high, Row<Z>::get(x[q], j));
+            if (high > mine) {
+                const float by_T = fast_exp2((mine - high) * per), by_1 = fast_exp2((mine - high) * kLog2e);
+#pragma unroll
+                for (int j = 0; j < E; ++j) { at_T[j] *= by_T; at_1[j] *= by_1; }
+                from = mine = high;
+            }
+            add(x[q]);
         }
     }
+    float m[2] = {t_mine, mine};
+    block_reduce<2, true, WAVES>(m, part);                  // (also: the list is there)
+    const float t_top = m[0], top = m[1];
+    const bool bad = t_top == INFINITY || label < -1 || label >= V;
+    const bool soft_part = t_top > -INFINITY && a.a < 1.f, hard_part = label >= 0 && a.a > 0.f;
+    for (int k = tid; k < a.K; k += THREADS) {
+        const int w = list.word[k];
+        if (w >= 0 && !bad) list.z[k] = Row<Z>::one(row + w);
+    }
+    const float z_label = !bad && label >= 0 ? Row<Z>::one(row + label) : 0.f;
+#pragma unroll
+    for (int j = E / 2; j; j /= 2)
+#pragma unroll
+        for (int i = 0; i < j; ++i) { at_T[i] += at_T[i + j]; at_1[i] += at_1[i + j]; }
+    // (a thread without a finite logit has sums of 0, or of NaN; the row's own maximum is infinite or there is nothing where `top` is)
+    const float down = mine > -INFINITY ? mine - top : 0.f;
+    float s[3] = {at_T[0] * fast_exp2(down * per), at_1[0] * fast_exp2(down * kLog2e), 0.f};
+    for (int k = tid; k < a.K; k += THREADS)
+        if (list.word[k] >= 0) s[2] += exponent.fine(list.q[k] - t_top);
+    block_reduce<3, false, WAVES>(s, part);
+    const float s_T = s[0], s_1 = FORM == kOne ? s[0] : s[1], t_sum = s[2];
+    const bool dead = !(s_T > 0.f);                         // a NaN, +infinity, or nothing finite
+    const float inv_T = dead ? quiet_nan() : 1.f / s_T, inv_1 = dead ? quiet_nan() : 1.f / s_1;
+    float l[1] = {0.f};
+    if (soft_part && !bad) {
+        const float log_sum = logf(s_T), log_t = logf(t_sum);
+        for (int k = tid; k < a.K; k += THREADS) {
+            if (list.word[k] < 0) continue;
+            const float d = list.q[k] - t_top, q = exponent.fine(d) / t_sum;
+            if (q > 0.f) l[0] += q * (d / a.T - log_t - (list.z[k] - top) / a.T + log_sum);
+            list.q[k] = q;
+        }
+    }
+    block_reduce<1, false, WAVES>(l, part);
+    if (tid == 0) {
+        a.loss[n] = row_loss(a, bad, soft_part, hard_part, dead, l[0], logf(s_1) - (z_label - top));
+        *reinterpret_cast<f32x4 *>(a.stats + 4ll * n) = f32x4{top, inv_T, inv_1, 0.f};
+    }
+    if (!GRAD) return;
+    const float g = a.row_weight ? a.row_weight[n] : 1.f;
+    const float k_T = soft_part ? g * (1.f - a.a) * a.T : 0.f, k_1 = hard_part ? g * a.a : 0.f;
+    const RowGrad<FORM == kTwo> grad(a, per, top, inv_T, inv_1, k_T, k_1, bad);
+    Z *out = static_cast<Z *>(a.grad) + n * a.grad_ld;
+    const int at = forget(tid);
+    if (grad.nothing()) {                                   // nothing is learned from the row, whatever it holds
+        const float zeros[E] = {};
+        for (int i = tid; i < vectors; i += THREADS) store_vector(out, i, zeros);
+        store_tail(out, V, 0.f);
+        return;
+    }
+    // what is read again first, the last of it in front: that is still in the L2
+    const int far_last = vectors > R * THREADS ? (vectors - R * THREADS - 1) / THREADS & ~3 : -1;
+    for (int f = far_last; f >= 0; f -= 4) {
+        u32x4 y[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const int i = (R + f + q) * THREADS + tid;
+            if (f + q < STASH) y[q] = stash[(f + q) * THREADS + tid];
+            else if (i < vectors) y[q] = load_vector(row, i);
+        }
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const int i = (R + f + q) * THREADS + tid;
+            float x[E];
+#pragma unroll
+            for (int j = 0; j < E; ++j) x[j] = grad(Row<Z>::get(y[q], j));
+            if (i < vectors) store_vector(out, i, x);
+        }
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        forget(v[r]);
+        float x[E];
+#pragma unroll
+        for (int j = 0; j < E; ++j) x[j] = grad(Row<Z>::get(v[r], j));
+        if (r * THREADS + at < vectors) store_vector(out, r * THREADS + at, x);
+    }
+    store_tail(out, V, grad(z_tail));
+    if (grad.dead) return;
+    const bool again = list.repeated<THREADS>();
+    seen_by_all();
+    const bool repeats = __syncthreads_or(again);
+    write_listed<Z, THREADS>(a, list, grad, out, 0, V, k_T, k_1, repeats, label, z_label);
+}
+
+// ---- rows in segments
+constexpr int kSegThreads = 256, kSegWaves = kSegThreads / 64, kMaxSegments = 64;
+// Of one segment: maximum m, sums relative to it at both temperatures, sum of q (z - m) and of q over the teacher's words in it, the label's
+// z - m.
+struct Part { float m, s_T, s_1, qz, q, label, pad[2]; };
+
+template <typename Z>
+__global__ __launch_bounds__(kSegThreads) void distill_part_kernel(DistillArgs a, int segments, int seg_len, int hash_size) {
+    constexpr int E = Row<Z>::E, WAVES = kSegWaves;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    __shared__ float part[5 * WAVES];
+    const int tid = threadIdx.x, n = blockIdx.x / segments, from = blockIdx.x % segments * seg_len, len = min(seg_len, a.V - from);
+    const Z *row = static_cast<const Z *>(a.logits) + n * a.ld;
+    const Exponent exponent(a.T);
+    const float per = exponent.per;
+    List list(lds, a.K, hash_size);
+    const int label = a.label ? a.label[n] : -1;
+    float m[2] = {list.read<kSegThreads>(a, n), -INFINITY};
+    const int vectors = len / E;
+    const float z_tail = load_tail(row + from, len);
+    m[1] = z_tail;
+    for (int i = tid; i < vectors; i += kSegThreads) {
+        const u32x4 x = load_vector(row + from, i);
+#pragma unroll
+        for (int j = 0; j < E; ++j) m[1] = fmaxf(m[1], Row<Z>::get(x, j));
+    }
+    block_reduce<2, true, WAVES>(m, part);
+    const float t_top = m[0], top = m[1];
+    const bool listed = t_top > -INFINITY && t_top < INFINITY;
+    float at_T[E] = {}, at_1[E] = {};
+    for (int i = tid; i < vectors; i += kSegThreads) {
+        const u32x4 x = load_vector(row + from, i);
+#pragma unroll
+        for (int j = 0; j < E; ++j) {
+            const float z = Row<Z>::get(x, j), d = z == -INFINITY ? -INFINITY : z - top;     // (top may be -infinity itself here)
+            at_T[j] += fast_exp2(d * per);
+            at_1[j] += fast_exp2(d * kLog2e);
+        }
+    }
+#pragma unroll
+    for (int j = E / 2; j; j /= 2)
+#pragma unroll
+        for (int i = 0; i < j; ++i) { at_T[i] += at_T[i + j]; at_1[i] += at_1[i + j]; }
+    const float d_tail = z_tail == -INFINITY ? -INFINITY : z_tail - top;
+    float s[5] = {at_T[0] + fast_exp2(d_tail * per), at_1[0] + fast_exp2(d_tail * kLog2e), 0.f, 0.f, 0.f};
+    if (listed)
+        for (int k = tid; k < a.K; k += kSegThreads)
+            if (list.word[k] >= 0) s[2] += exponent.fine(list.q[k] - t_top);
+    block_reduce<5, false, WAVES>(s, part);
+    const float t_sum = s[2];
+    float d[2] = {0.f, 0.f};
+    if (listed)
+        for (int k = tid; k < a.K; k += kSegThreads) {
+            const int w = list.word[k];
+            if (w < from || w >= from + len) continue;
+            const float q = exponent.fine(list.q[k] - t_top) / t_sum, z = Row<Z>::one(row + w);
+            if (q > 0.f) { d[0] += q * (z == -INFINITY ? -INFINITY : z - top); d[1] += q; }
+        }
+    block_reduce<2, false, WAVES>(d, part);
+    if (tid == 0) {
+        Part p = {top, s[0], s[1], d[0], d[1], 0.f, {0.f, 0.f}};
+        if (label >= from && label < from + len) { const float z = Row<Z>::one(row + label); p.label = z == -INFINITY ? -INFINITY : z - top; }
+        static_cast<Part *>(a.ws)[blockIdx.x] = p;
+    }
+}
+
+// BACKWARD: statistics from memory, else from the segments' parts (then the row's first segment writes loss and statistics).
+template <typename Z, bool BACKWARD, bool TWO>
+__global__ __launch_bounds__(kSegThreads) void distill_segment_kernel(DistillArgs a, int parts, int part_len, int segments, int seg_len, int hash_size) {
+    constexpr int E = Row<Z>::E, WAVES = kSegWaves, R = 4;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    __shared__ float part[2 * WAVES];
+    const int tid = threadIdx.x, lane = tid & 63, n = blockIdx.x / segments, seg = blockIdx.x % segments, from = seg * seg_len, V = a.V;
+    const int len = a.grad ? min(seg_len, V - from) : 0, vectors = len / E;
+    const Z *row = static_cast<const Z *>(a.logits) + n * a.ld;
+    const Exponent exponent(a.T);
+    const float per = exponent.per;
+    List list(lds, a.K, hash_size);
+    const int label = a.label ? a.label[n] : -1;
+    float m[1] = {list.read<kSegThreads>(a, n)};
+    u32x4 first[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        first[r] = Row<Z>::nothing();
+        if (r * kSegThreads + tid < vectors) first[r] = load_vector(row + from, r * kSegThreads + tid);
+    }
+    const float z_tail = load_tail(row + from, len);
+    block_reduce<1, true, WAVES>(m, part);
+    const float t_top = m[0];
+    const bool bad = t_top == INFINITY || label < -1 || label >= V;
+    const bool soft_part = t_top > -INFINITY && a.a < 1.f, hard_part = label >= 0 && a.a > 0.f;
+    float s[1] = {0.f};
+    for (int k = tid; k < a.K; k += kSegThreads) {
+        const int w = list.word[k];
+        if (w < 0 || bad) continue;
+        s[0] += exponent.fine(list.q[k] - t_top);
+        if (w >= from && w < from + len) list.z[k] = Row<Z>::one(row + w);
+    }
+    const float z_label = !bad && label >= from && label < from + len ? Row<Z>::one(row + label) : 0.f;
+    block_reduce<1, false, WAVES>(s, part);
+    const float t_sum = s[0];
+    float entropy[1] = {0.f};
+    if (soft_part && !bad) {
+        const float log_t = logf(t_sum);
+        for (int k = tid; k < a.K; k += kSegThreads) {
+            if (list.word[k] < 0) continue;
+            const float d = list.q[k] - t_top, q = exponent.fine(d) / t_sum;
+            if (q > 0.f) entropy[0] += q * (d / a.T - log_t);
+            list.q[k] = q;
+        }
+    }
+    float top, inv_T, inv_1;
+    if (BACKWARD) {
+        top = a.stats[4ll * n];
+        inv_T = a.stats[4ll * n + 1];
+        inv_1 = a.stats[4ll * n + 2];
+    } else {
+        Part p = {-INFINITY, 0.f, 0.f, 0.f, 0.f, 0.f, {0.f, 0.f}};          // every wave joins them for itself
+        if (lane < parts) p = static_cast<const Part *>(a.ws)[(long long)n * parts + lane];
+        top = wave_max(p.m);
+        const bool some = p.m > -INFINITY;
+        const float d = p.m - top;
+        const float s_T = wave_sum(some ? p.s_T * fast_exp2(d * per) : p.s_T), s_1 = wave_sum(some ? p.s_1 * fast_exp2(d * kLog2e) : p.s_1);
+        const bool dead = !(s_T > 0.f) || top == INFINITY;
+        inv_T = dead ? quiet_nan() : 1.f / s_T;
+        inv_1 = dead ? quiet_nan() : 1.f / s_1;
+        if (seg == 0) {
+            block_reduce<1, false, WAVES>(entropy, part);
+            const float qz = wave_sum(p.q > 0.f ? p.qz + p.q * d : 0.f), q = wave_sum(p.q);
+            const float z_minus = wave_sum(hard_part && !bad && label / part_len == lane ? p.label + (some ? d : 0.f) : 0.f);
+            if (tid == 0) {
+                a.loss[n] = row_loss(a, bad, soft_part, hard_part, dead, entropy[0] - qz / a.T + q * logf(s_T), logf(s_1) - z_minus);
+                *reinterpret_cast<f32x4 *>(a.stats + 4ll * n) = f32x4{top, inv_T, inv_1, 0.f};
+            }
+        }
+    }
+    if (len == 0) return;
+    const float g = a.row_weight ? a.row_weight[n] : 1.f;
+    const float k_T = soft_part ? g * (1.f - a.a) * a.T : 0.f, k_1 = hard_part ? g * a.a : 0.f;
+    const RowGrad<TWO> grad(a, per, top, inv_T, inv_1, k_T, k_1, bad);
+    Z *out = static_cast<Z *>(a.grad) + n * a.grad_ld + from;
+    if (grad.nothing()) {
+        const float zeros[E] = {};
+        for (int i = tid; i < vectors; i += kSegThreads) store_vector(out, i, zeros);
+        store_tail(out, len, 0.f);
+        return;
+    }
+    __syncthreads();                                        // every place of the list that is in this segment has been read
+    auto put = [&](int i, u32x4 y) {
+        float x[E];
+#pragma unroll
+        for (int j = 0; j < E; ++j) x[j] = grad(Row<Z>::get(y, j));
+        store_vector(out, i, x);
+    };
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+        if (r * kSegThreads + tid < vectors) put(r * kSegThreads + tid, first[r]);
+    for (int i = R * kSegThreads + tid; i < vectors; i += kSegThreads) put(i, load_vector(row + from, i));
+    store_tail(out, len, grad(z_tail));
+    if (grad.dead) return;
+    const bool again = list.repeated<kSegThreads>();
+    seen_by_all();
+    const bool repeats = __syncthreads_or(again);
+    write_listed<Z, kSegThreads>(a, list, grad, out - from, from, len, k_T, k_1, repeats, label, z_label);
+}
+
+int hash_size_of(int K) {
+    int h = 16;
+    while (h < 2 * K) h <<= 1;
+    return h;
+}
+size_t list_bytes(int K) { return (size_t)K * 12 + (size_t)hash_size_of(K) * 4; }
+
+Form form_of(const DistillArgs &a) { return a.T == 1.f ? kOne : a.a > 0.f && a.a < 1.f ? kTwo : kTwoSums; }
+
+template <typename Z, int THREADS, int R, int STASH, bool GRAD, Form FORM>
+hipError_t launch_row_kernel(const DistillArgs &a, hipStream_t stream) {
+    static LdsLimit limit;
+    const size_t bytes = list_bytes(a.K) + (size_t)STASH * THREADS * 16;
+    const auto kernel = distill_row_kernel<Z, THREADS, R, STASH, GRAD, FORM>;
+    const hipError_t e = limit.ensure(reinterpret_cast<const void *>(kernel), bytes);
+    if (e != hipSuccess) return e;
+    kernel<<<a.N, THREADS, bytes, stream>>>(a, hash_size_of(a.K));
+    return hipGetLastError();
+}
+template <typename Z, int THREADS, int R, int STASH>
+hipError_t launch_rows(const DistillArgs &a, hipStream_t stream) {
+    const Form form = form_of(a);
+    if (!a.grad) return form == kOne ? launch_row_kernel<Z, THREADS, R, 0, false, kOne>(a, stream) : launch_row_kernel<Z, THREADS, R, 0, false, kTwoSums>(a, stream);
+    if (form == kOne) return launch_row_kernel<Z, THREADS, R, STASH, true, kOne>(a, stream);
+    return form == kTwo ? launch_row_kernel<Z, THREADS, R, STASH, true, kTwo>(a, stream) : launch_row_kernel<Z, THREADS, R, STASH, true, kTwoSums>(a, stream);
+}
+template <typename Z, bool BACKWARD, bool TWO>
+hipError_t launch_segments(const DistillArgs &a, int parts, int part_len, int segments, int seg_len, hipStream_t stream) {
+    static LdsLimit limit;
+    const size_t bytes = list_bytes(a.K);
+    const auto kernel = distill_segment_kernel<Z, BACKWARD, TWO>;
+    const hipError_t e = limit.ensure(reinterpret_cast<const void *>(kernel), bytes);
+    if (e != hipSuccess) return e;
+    const long long groups = (long long)a.N * segments;
+    if (groups > 0x7FFFFFFF) return hipErrorInvalidValue;
+    kernel<<<(unsigned)groups, kSegThreads, bytes, stream>>>(a, parts, part_len, segments, seg_len, hash_size_of(a.K));
+    return hipGetLastError();
+}
+
+// Segments of a row: how many, and their length (a multiple of a vector).
+struct Cut { int segments, len; };
+Cut cut_row(int V, int E, int segments) {
+    const int vectors = (V + E - 1) / E, per = (vectors + segments - 1) / segments;
+    return Cut{(vectors + per - 1) / per, per * E};
+}
+
+// Rows too few to fill the chip by one workgroup each, and long enough to cut.
+int segments_of(int N, int V) {
+    if (N >= 128 || V < 8192) return 1;
+    int s = 2 * kChipGroups / N;
+    if (s > V / 4096) s = V / 4096;
+    return s < 2 ? 1 : s > kMaxSegments ? kMaxSegments : s;
+}
+
+template <typename Z>
+hipError_t forward(const DistillArgs &a, hipStream_t stream) {
+    constexpr int E = Row<Z>::E;
+    const int s = segments_of(a.N, a.V);
+    if (s > 1) {
+        static LdsLimit limit;
+        const size_t bytes = list_bytes(a.K);
+        const Cut cut = cut_row(a.V, E, s);
+        const hipError_t e = limit.ensure(reinterpret_cast<const void *>(distill_part_kernel<Z>), bytes);
+        if (e != hipSuccess) return e;
+        distill_part_kernel<Z><<<a.N * cut.segments, kSegThreads, bytes, stream>>>(a, cut.segments, cut.len, hash_size_of(a.K));
+        const int to_write = a.grad ? cut.segments : 1;
+        return form_of(a) == kTwo ? launch_segments<Z, false, true>(a, cut.segments, cut.len, to_write, cut.len, stream)
+                                  : launch_segments<Z, false, false>(a, cut.segments, cut.len, to_write, cut.len, stream);
+    }
+    const int vectors = (a.V + E - 1) / E;
+    if (vectors <= 256 * 4) return launch_rows<Z, 256, 4, 0>(a, stream);
+    if (vectors <= 512 * 8) return launch_rows<Z, 512, 8, 0>(a, stream);
+    if (vectors <= 512 * 16) return launch_rows<Z, 512, 16, 0>(a, stream);
+    if (vectors <= 1024 * 16 || !a.grad || list_bytes(a.K) > 28 * 1024) return launch_rows<Z, 1024, 16, 0>(a, stream);
+    return launch_rows<Z, 1024, E == 4 ? 20 : 16, 8>(a, stream);
+}
+
+template <typename Z>
+hipError_t backward(const DistillArgs &a, hipStream_t stream) {
+    const Cut cut = cut_row(a.V, Row<Z>::E, (a.V + 8191) / 8192);
+    return form_of(a) == kTwo ? launch_segments<Z, true, true>(a, 0, 1, cut.segments, cut.len, stream) : launch_segments<Z, true, false>(a, 0, 1, cut.segments, cut.len, stream);
 }
 
 }  // namespace
 
-size_t distill_workspace_bytes(int N, int V) { return 256; }
+size_t distill_workspace_bytes(int N, int V) {
+    const int s = segments_of(N, V);
+    return s > 1 ? (size_t)N * s * sizeof(Part) : 16;
+}
 
-hipError_t launch_distill(const DistillArgs &a, hipStream_t stream) {
-    distill_plain_kernel<<<a.N < 65535 ? a.N : 65535, kThreads, 0, stream>>>(a, true);
-    return hipGetLastError();
-}
-hipError_t launch_distill_backward(const DistillArgs &a, hipStream_t stream) {
-    distill_plain_kernel<<<a.N < 65535 ? a.N : 65535, kThreads, 0, stream>>>(a, false);
-    return hipGetLastError();
-}
+hipError_t launch_distill(const DistillArgs &a, hipStream_t stream) { return a.bf16 ? forward<uint16_t>(a, stream) : forward<float>(a, stream); }
+hipError_t launch_distill_backward(const DistillArgs &a, hipStream_t stream) { return a.bf16 ? backward<uint16_t>(a, stream) : backward<float>(a, stream); }
 
 }  // namespace rnnlm
