@@ -24,20 +24,32 @@ __device__ __forceinline__ uint32_t key_of(float z) {
 }
 __device__ __forceinline__ float of_key(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k); }
 
+// Values that all lanes share, in scalar registers.
+__device__ __forceinline__ uint32_t uniform(uint32_t x) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)x); }
+__device__ __forceinline__ float uniform(float x) { return __uint_as_float(uniform(__float_as_uint(x))); }
+__device__ __forceinline__ u64 uniform(u64 x) { return (u64)uniform((uint32_t)(x >> 32)) << 32 | uniform((uint32_t)x); }
+__device__ __forceinline__ double uniform(double x) { return __longlong_as_double((long long)uniform((u64)__double_as_longlong(x))); }
+
+// a * b + c with c in scalar registers (the compiler copies it into a vector register in front of every use)
+__device__ __forceinline__ double fma_with(double a, double b, double c) {
+    double r;
+    asm("v_fma_f64 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "s"(c));
+    return r;
+}
+
 // 2^y for y <= 0 as a whole number of 2^-bits, to nearest (bits <= 50; anything below -200 is nothing).  2^f on [-1/2, 1/2] is 1 + f times a
 // polynomial fitted for the least relative error, 1.5e-14; the product with 2^bits is rounded by adding 2^52, below which its last bit counts 1.
 __device__ __forceinline__ u64 fixed_exp2(double y, int bits) {
     y = fmax(y, -200.0);
     const double n = rint(y), f = y - n;
-    double q = 0x1.b3de2c7e1dde3p-24;
-    q = fma(q, f, 0x1.63e69680bde3cp-20);
-    q = fma(q, f, 0x1.ffce2fc63d69ep-17);
-    q = fma(q, f, 0x1.430897f31267cp-13);
-    q = fma(q, f, 0x1.5d87fd9386691p-10);
-    q = fma(q, f, 0x1.3b2ab72412393p-7);
-    q = fma(q, f, 0x1.c6b08d70c8822p-5);
-    q = fma(q, f, 0x1.ebfbdff81be04p-3);
-    q = fma(q, f, 0x1.62e42fefa37d1p-1);
+    double q = fma_with(0x1.b3de2c7e1dde3p-24, f, 0x1.63e69680bde3cp-20);
+    q = fma_with(q, f, 0x1.ffce2fc63d69ep-17);
+    q = fma_with(q, f, 0x1.430897f31267cp-13);
+    q = fma_with(q, f, 0x1.5d87fd9386691p-10);
+    q = fma_with(q, f, 0x1.3b2ab72412393p-7);
+    q = fma_with(q, f, 0x1.c6b08d70c8822p-5);
+    q = fma_with(q, f, 0x1.ebfbdff81be04p-3);
+    q = fma_with(q, f, 0x1.62e42fefa37d1p-1);
     q = fma(q, f, 1.0);
     return (u64)__double_as_longlong(ldexp(q, (int)n + bits) + 0x1p52) - 0x4330000000000000ull;
 }
@@ -206,9 +218,11 @@ __global__ __launch_bounds__(kThreads) void sample_plain_kernel(SampleArgs a, in
 
 // ---- A row in the registers of one workgroup
 
-constexpr int kBins = 2048;                  // of the distance to the row's maximum, kBins / 64 to a factor of two in weight
-constexpr int kList = 2048;                  // words that can be sorted
-constexpr float kBinsPerOctave = kBins / 64;
+// Bins of the distance to the row's maximum, over the kOctaves factors of two in which a weight is not nothing; words that can be listed;
+// words that are put in order by comparing each with each.
+constexpr int kOctaves = 52, kSmall = 256;
+constexpr int bins_of(int threads) { return threads > 256 ? 4096 : 1024; }
+constexpr int list_of(int threads) { return threads > 256 ? 2048 : 512; }
 
 typedef u32x4 u32x4_any __attribute__((aligned(2)));
 typedef uint32_t u32x16 __attribute__((ext_vector_type(16)));
@@ -262,127 +276,64 @@ template <> struct RowOf<uint16_t> {
     static __device__ __forceinline__ uint32_t pack(const float (&z)[8], int i) { return __float_as_uint(z[2 * i]) >> 16 | (__float_as_uint(z[2 * i + 1]) & 0xFFFF0000u); }   // (bfloat16 values)
 };
 
-__device__ __forceinline__ u64 wave_scan64(u64 v, int lane) {                // inclusive
-#pragma unroll
-    for (int s = 1; s < 64; s <<= 1) { const u64 o = __shfl_up(v, s); if (lane >= s) v += o; }
-    return v;
+// Inclusive prefix sums over the wave in registers, as wave_inclusive_scan.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ u64 moved(u64 v) {
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)v, CTRL, ROWS, 0xF, false);
+    const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(v >> 32), CTRL, ROWS, 0xF, false);
+    return (u64)hi << 32 | lo;
+}
+__device__ __forceinline__ u64 wave_scan64(u64 v) {
+    v += moved<0x111, 0xF>(v);
+    v += moved<0x112, 0xF>(v);
+    v += moved<0x114, 0xF>(v);
+    v += moved<0x118, 0xF>(v);
+    v += moved<0x142, 0xA>(v);
+    return v + moved<0x143, 0xC>(v);
+}
+__device__ __forceinline__ u64 last_lane(u64 v) {
+    return (u64)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(v >> 32), 63) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, 63);
 }
 // Order of the words: larger logits first, equal ones by rising id.
 __device__ __forceinline__ u64 place(float z, uint32_t id) { return (u64)key_of(z + 0.f) << 32 | (uint32_t)~id; }
 __device__ __forceinline__ float logit_of(u64 place) { return of_key((uint32_t)(place >> 32)); }
 
+template <int THREADS>
 struct Shared {
-    u64 weight[kBins];                       // histogram; weights of the listed words
-    u64 list[kList];
-    int count[kBins];
-    u64 wave64[16];
+    union {                                  // histogram
+        u64 weight[bins_of(THREADS)];
+        int count[bins_of(THREADS)];
+    };
+    u64 list[list_of(THREADS)];
+    u64 small[kSmall], small_w[kSmall];
+    u64 wave64[16], low64[16], high64[16];
     float wavef[16];
-    u64 want, total, found_w, border;
-    int bin, n, word, m;
+    u64 want, found_w, border;
+    int bin, n, word;
 };
 
+// Inclusive over the threads.
 template <int THREADS>
-__device__ __forceinline__ u64 block_scan64(u64 v, Shared &sh, u64 &total) {  // inclusive over the threads
+__device__ __forceinline__ u64 block_scan64(u64 v, Shared<THREADS> &sh, u64 &total) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    v = wave_scan64(v, lane);
+    v = wave_scan64(v);
     __syncthreads();
     if (lane == 63) sh.wave64[wave] = v;
     __syncthreads();
-    u64 before = 0, all = 0;
-#pragma unroll
-    for (int w = 0; w < THREADS / 64; ++w) {
-        const u64 x = sh.wave64[w];
-        if (w < wave) before += x;
-        all += x;
-    }
-    total = all;
-    return v + before;
-}
-
-// list[0 .. n) in falling (or rising) order, padded to a power of two with what comes last.  Exchanges over up to 64 places stay in one
-// wave's 128 and need no barrier.
-template <int THREADS, bool FALLING>
-__device__ __forceinline__ void sort_list(u64 *list, int n) {
-    int P = 2;
-    while (P < n) P <<= 1;
-    for (int i = n + threadIdx.x; i < P; i += THREADS) list[i] = FALLING ? 0 : ~0ull;
-    __syncthreads();
-    for (int size = 2; size <= P; size <<= 1)
-        for (int stride = size >> 1; stride; stride >>= 1) {
-            for (int i = threadIdx.x; i < P / 2; i += THREADS) {
-                const int a = 2 * i - (i & (stride - 1)), b = a + stride;
-                const u64 x = list[a], y = list[b];
-                const bool falls = ((a & size) == 0) == FALLING;
-                if (falls ? x < y : x > y) { list[a] = y; list[b] = x; }
-            }
-            if (stride > 64 || (stride == 1 && size >= 128)) __syncthreads();
-            else __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");
-        }
-    __syncthreads();
-}
-
-// The limits and the draw on n listed words, among them all that can be kept: top_k of them (all: n), then top-p, min-p, and the draw in the
-// order of the ids.
-template <int THREADS>
-__device__ __forceinline__ void draw_from_list(Shared &sh, int n, int top_k, float p, u64 least, float u, const Weight &weight) {
-    constexpr int M = kList / THREADS;
-    const int tid = threadIdx.x;
-    if (top_k > n) top_k = n;
-    sort_list<THREADS, true>(sh.list, n);
-    u64 w[M], sum = 0, total;
-#pragma unroll
-    for (int i = 0; i < M; ++i) {
-        const int at = tid * M + i;
-        w[i] = at < top_k ? weight(logit_of(sh.list[at])) : 0;
-        sum += w[i];
-    }
-    if (tid == 0) { sh.m = top_k; sh.n = top_k; }
-    u64 upto = block_scan64<THREADS>(sum, sh, total) - sum;
-    u64 want = p > 0.f ? (u64)ceil((double)p * (double)total) : 1;
-    if (want < 1) want = 1;
-    u64 keep[M];
-#pragma unroll
-    for (int i = 0; i < M; ++i) {
-        const int at = tid * M + i;
-        const u64 before = upto;
-        upto += w[i];
-        if (at < top_k) {
-            if (p < 1.f && before < want && upto >= want) sh.m = at + 1;
-            if (w[i] < least) atomicMin(&sh.n, at);
-            sh.weight[at] = w[i];
-        }
-        keep[i] = at < top_k ? (u64)(uint32_t)~(uint32_t)sh.list[at] << 32 | (uint32_t)at : 0;
-    }
-    __syncthreads();
-    const int m = min(sh.m, sh.n);
-#pragma unroll
-    for (int i = 0; i < M; ++i)
-        if (tid * M + i < m) sh.list[tid * M + i] = keep[i];
-    __syncthreads();
-    sort_list<THREADS, false>(sh.list, m);
-    sum = 0;
-#pragma unroll
-    for (int i = 0; i < M; ++i) {
-        const int at = tid * M + i;
-        w[i] = at < m ? sh.weight[(uint32_t)sh.list[at]] : 0;
-        sum += w[i];
-    }
-    upto = block_scan64<THREADS>(sum, sh, total) - sum;
-    const u64 target = (u64)floor((double)u * (double)total);
-#pragma unroll
-    for (int i = 0; i < M; ++i) {
-        const u64 before = upto;
-        upto += w[i];
-        if (before <= target && target < upto) { sh.word = (int)(sh.list[tid * M + i] >> 32); sh.found_w = w[i]; sh.total = total; }
-    }
-    __syncthreads();
+    const u64 all = wave_scan64(lane < THREADS / 64 ? sh.wave64[lane] : 0);
+    total = last_lane(all);
+    const int before = __builtin_amdgcn_readfirstlane(wave) - 1;
+    const uint32_t lo = before < 0 ? 0 : (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)all, before);
+    const uint32_t hi = before < 0 ? 0 : (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(all >> 32), before);
+    return v + ((u64)hi << 32 | lo);
 }
 
 template <typename Z, int THREADS, int R>
 __global__ __launch_bounds__(THREADS, 4) void sample_row_kernel(SampleArgs a, int bits) {
     typedef RowOf<Z> O;
-    constexpr int E = O::E, WAVES = THREADS / 64, kPerThread = kBins / THREADS;
-    __shared__ Shared sh;
+    constexpr int E = O::E, WAVES = THREADS / 64, kBins = bins_of(THREADS), kList = list_of(THREADS), kPerThread = kBins / THREADS;
+    constexpr float kBinsPerOctave = (float)kBins / kOctaves;
+    __shared__ Shared<THREADS> sh;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = blockIdx.x, V = a.V;
     const Z *row = static_cast<const Z *>(a.logits) + n * a.ld;
     const float T = a.temperature ? a.temperature[n] : 1.f, p = a.top_p ? a.top_p[n] : 1.f, mp = a.min_p ? a.min_p[n] : 0.f, u = a.u[n];
@@ -432,7 +383,7 @@ __global__ __launch_bounds__(THREADS, 4) void sample_row_kernel(SampleArgs a, in
             for (int j = 0; j < E; ++j) f(O::get(x, j), (uint32_t)((first + r * 64) * E + j));
         });
     };
-    for (int i = tid; i < kBins; i += THREADS) { sh.count[i] = 0; sh.weight[i] = 0; }
+    for (int i = tid; i < kBins; i += THREADS) sh.count[i] = 0;
     if (tid == 0) sh.n = 0;
     float mine = -INFINITY;
     bool nan = false;
@@ -440,8 +391,7 @@ __global__ __launch_bounds__(THREADS, 4) void sample_row_kernel(SampleArgs a, in
     float top = wave_max(mine);
     if (lane == 0) sh.wavef[wave] = top;
     const bool bad = __syncthreads_or(nan || !(T >= 0.f) || T == INFINITY || !(u >= 0.f && u < 1.f) || p != p || mp != mp);
-#pragma unroll
-    for (int w = 0; w < WAVES; ++w) top = fmaxf(top, sh.wavef[w]);
+    top = uniform(wave_max(lane < WAVES ? sh.wavef[lane] : -INFINITY));
     if (bad || top == -INFINITY) {
         if (tid == 0) { a.word[n] = -1; if (a.logprob) a.logprob[n] = quiet_nan(); }
         return;
@@ -450,7 +400,7 @@ __global__ __launch_bounds__(THREADS, 4) void sample_row_kernel(SampleArgs a, in
         if (tid == 0) sh.word = 0x7FFFFFFF;
         __syncthreads();
         uint32_t at = 0x7FFFFFFF;
-        if (mine == top) each([&](float z, uint32_t id) { if (z == top && id < at) at = id; });
+        if (__any(mine == top)) each([&](float z, uint32_t id) { at = z == top && id < at ? id : at; });
         if (at != 0x7FFFFFFF) atomicMin(&sh.word, (int)at);
         __syncthreads();
         if (tid == 0) { a.word[n] = sh.word; if (a.logprob) a.logprob[n] = 0.f; }
@@ -461,21 +411,30 @@ __global__ __launch_bounds__(THREADS, 4) void sample_row_kernel(SampleArgs a, in
         mine = mine == INFINITY ? 0.f : -INFINITY;
         top = 0.f;
     }
-    const Weight weight{(double)top, 1.4426950408889634 / (double)T, bits};
-    const float bin_scale = fminf((float)(weight.per * kBinsPerOctave), 3.4e38f);
+    const Weight weight{uniform((double)top), uniform(1.4426950408889634 / (double)T), bits};
+    const float bin_scale = uniform(fminf((float)(weight.per * kBinsPerOctave), 3.4e38f));
     auto bin_of = [&](float z) {                              // rises as z falls; what is in the last one weighs nothing
         const float x = (top - z) * bin_scale;
         return x < (float)(kBins - 1) ? (int)x : kBins - 1;
     };
-    const u64 least = mp > 0.f ? (u64)ceil((double)fminf(mp, 1.f) * (double)weight.one()) : 0;
-    // Appends words to the list; beyond kList they are only counted.
-    auto append = [&](bool take, float z, uint32_t id) {
-        const u64 who = __ballot(take);
-        if (who == 0) return;
+    const u64 least = mp > 0.f ? uniform((u64)ceil((double)fminf(mp, 1.f) * (double)weight.one())) : 0;
+    // Appends words to a list, `to` of at most `most`; beyond that they are only counted.  M words of a thread at once.
+    auto append = [&](auto take, auto put, int most) {
         int at = 0;
-        if (lane == 0) at = atomicAdd(&sh.n, __popcll(who));
-        at = __builtin_amdgcn_readfirstlane(at) + __popcll(who & ((1ull << lane) - 1));
-        if (take && at < kList) sh.list[at] = place(z, id);
+        constexpr int M = sizeof(take) / sizeof(bool);
+        u64 who[M];
+        int all = 0;
+#pragma unroll
+        for (int i = 0; i < M; ++i) { who[i] = __ballot(take.is[i]); all += __popcll(who[i]); }
+        if (all == 0) return;
+        if (lane == 0) at = atomicAdd(&sh.n, all);
+        at = __builtin_amdgcn_readfirstlane(at);
+#pragma unroll
+        for (int i = 0; i < M; ++i) {
+            const int mine_at = at + __popcll(who[i] & ((1ull << lane) - 1));
+            if (take.is[i] && mine_at < most) put(i, mine_at);
+            at += __popcll(who[i]);
+        }
     };
     // The bin where `want` of the histogram (counts, or weights) is reached from the front, and what is still wanted of that bin.
     auto find_bin = [&](bool by_weight, u64 want) {
@@ -487,178 +446,210 @@ __global__ __launch_bounds__(THREADS, 4) void sample_row_kernel(SampleArgs a, in
         }
         if (tid == 0) sh.bin = kBins - 1;
         u64 upto = block_scan64<THREADS>(sum, sh, total) - sum;
+        if (upto < want && upto + sum >= want) {
 #pragma unroll
-        for (int i = 0; i < kPerThread; ++i) {
-            if (upto < want && upto + h[i] >= want) { sh.bin = tid * kPerThread + i; sh.want = want - upto; }
-            upto += h[i];
+            for (int i = 0; i < kPerThread; ++i) {
+                if (upto < want && upto + h[i] >= want) { sh.bin = tid * kPerThread + i; sh.want = want - upto; }
+                upto += h[i];
+            }
         }
         __syncthreads();
     };
-    auto finish = [&](int word, u64 w, u64 total) {
-        if (tid == 0) { a.word[n] = word; if (a.logprob) a.logprob[n] = (float)log((double)w / (double)total); }
-    };
 
+    // Few words kept: they are listed.  The top_k-th largest of the threads' own maxima is no more than the top_k-th largest logit, so whatever
+    // lies in its bin or in front of it is enough.
     const bool few = k > 0 && k < V;
-    // Few words, or few of them kept: all that can be kept fit the list.  The top_k-th largest of the threads' own maxima is no more than the
-    // top_k-th largest logit, so whatever lies in its bin or in front of it is enough.
-    if (V <= kList || (few && k <= THREADS / 2)) {
-        int edge = kBins - 1;
-        if (V > kList) {
-            if (mine > -INFINITY) atomicAdd(&sh.count[bin_of(mine)], 1);
-            __syncthreads();
-            find_bin(false, (u64)k);
-            edge = sh.bin;
-        }
-        if (V <= kList || edge < kBins - 1) {
-            if (V <= kList) each([&](float z, uint32_t id) { append(z > -INFINITY, z, id); });
-            else {
-                // floats in front of the bin's far edge; the edge itself is checked by the bin
-                each([&](float z, uint32_t id) { append((top - z) * bin_scale < (float)(edge + 1), z, id); });
-            }
-            __syncthreads();
-            const int listed = sh.n;
-            if (listed <= kList) {
-                __syncthreads();
-                draw_from_list<THREADS>(sh, listed, few ? k : listed, p, least, u, weight);
-                finish(sh.word, sh.found_w, sh.total);
-                return;
-            }
-        }
+    bool in_list = false;
+    int listed = 0;
+    if (few && k <= THREADS / 2) {
+        if (mine > -INFINITY) atomicAdd(&sh.count[bin_of(mine)], 1);
         __syncthreads();
-        for (int i = tid; i < kBins; i += THREADS) sh.count[i] = 0;
-        __syncthreads();
+        find_bin(false, (u64)k);
+        const int edge = sh.bin;
+        if (edge < kBins - 1) {
+            each_vector([&](int r, u32x4 x) {
+                struct { bool is[E]; } take;
+#pragma unroll
+                for (int j = 0; j < E; ++j) take.is[j] = (top - O::get(x, j)) * bin_scale < (float)(edge + 1);
+                append(take, [&](int j, int to) { sh.list[to] = place(O::get(x, j), (uint32_t)((first + r * 64) * E + j)); }, kList);
+            });
+            __syncthreads();
+            listed = sh.n;
+            in_list = listed <= kList;
+        }
     }
+    auto over = [&](auto f) {                                 // the listed words, or all
+        if (in_list)
+            for (int i = tid; i - tid < listed; i += THREADS) {
+                const u64 w = i < listed ? sh.list[i] : 0;
+                f(i < listed, logit_of(w), (uint32_t)~(uint32_t)w);
+            }
+        else each([&](float z, uint32_t id) { f(id < (uint32_t)V, z, id); });
+    };
 
-    // All words: limits as the place of the last word kept.
-    u64 border = 0;
-    auto kept = [&](float z, uint32_t id) { return place(z, id) >= border; };
-    // The shortest prefix that reaches `want` words or weight (of the histogram that is there, by distance): the new border.
-    auto cut = [&](bool by_weight, u64 want) {
+    // Limits as the place of the last word kept: top_k, top_p, and of listed words the draw as well, which is the same search in the order of
+    // the ids.  Each by a histogram, the bin in which what is wanted is reached, and that bin's words.
+    u64 border = 0, total = 0;
+    int id_shift = 0;
+    while (V >> id_shift >= kBins) ++id_shift;
+#pragma unroll 1
+    for (int stage = 0; stage < 3; ++stage) {
+        if (stage == 0 ? !few : stage == 1 ? !(p < 1.f) : !in_list) continue;
+        const bool by_weight = stage > 0, by_id = stage == 2;
+        auto weigh = [&](float z) {
+            const u64 w = by_weight ? weight(z) : 1;
+            return by_id && w < least ? 0 : w;
+        };
+        auto bin_at = [&](float z, uint32_t id) { return by_id ? (int)(id >> id_shift) : bin_of(z); };
+        auto order = [&](float z, uint32_t id) { return by_id ? ~(u64)id : place(z, id); };          // falls from word to word
+        auto is_kept = [&](float z, uint32_t id) { return z > -INFINITY && place(z, id) >= border; };
+        __syncthreads();
+        for (int i = tid; i < kBins; i += THREADS) sh.weight[i] = 0;
+        __syncthreads();
+        u64 sum = 0;
+        if (by_weight) over([&](bool is, float z, uint32_t id) {
+            u64 w = weight(z);
+            w = is && is_kept(z, id) && !(by_id && w < least) ? w : 0;
+            sum += w;
+            if (w) atomicAdd(&sh.weight[bin_at(z, id)], w);
+        });
+        else over([&](bool is, float z, uint32_t id) {
+            if (is && is_kept(z, id)) atomicAdd(&sh.count[bin_at(z, id)], 1);
+        });
+        block_scan64<THREADS>(sum, sh, total);
+        u64 want = (u64)k;
+        if (stage == 1) { want = p > 0.f ? (u64)ceil((double)p * (double)total) : 1; if (want < 1) want = 1; }
+        if (stage == 2) want = (u64)floor((double)u * (double)total) + 1;
         find_bin(by_weight, want);
         const int bin = sh.bin;
-        if (bin == kBins - 1) return;                         // beyond it nothing has a weight
+        if (bin == kBins - 1 && !by_id) continue;             // beyond it nothing has a weight
         want = sh.want;
-        uint32_t low = 0, high = 0xFFFFFFFFu, id_low = 0, id_high = 0xFFFFFFFFu;      // of the keys, and of the ids where only one key is left
-        auto inside = [&](float z, uint32_t id) {
-            const uint32_t key = key_of(z + 0.f);
-            return bin_of(z) == bin && key >= low && key <= high && id >= id_low && id <= id_high && kept(z, id);
+        u64 low = 0, high = ~0ull;                            // of the orders
+        // (most vectors have no word of one bin)
+        auto inside = [&](bool is, float z, uint32_t id) {
+            bool yes = is && bin_at(z, id) == bin;
+            if (!__any(yes)) return false;
+            const u64 o = order(z, id);
+            return yes && is_kept(z, id) && o >= low && o <= high;
         };
         while (true) {
             __syncthreads();
             if (tid == 0) sh.n = 0;
             __syncthreads();
-            each([&](float z, uint32_t id) { append(inside(z, id), z, id); });
+            u64 least_o = ~0ull, most_o = 0;
+            over([&](bool is, float z, uint32_t id) {
+                struct { bool is[1]; } take = {{inside(is, z, id)}};
+                if (!__any(take.is[0])) return;
+                const u64 o = order(z, id);
+                if (take.is[0]) { least_o = o < least_o ? o : least_o; most_o = o > most_o ? o : most_o; }
+                append(take, [&](int, int to) { sh.small[to] = o; sh.small_w[to] = weigh(z); }, kSmall);
+            });
             __syncthreads();
-            const int listed = sh.n;
-            if (listed <= kList) {
+            const int some = sh.n;
+            if (some <= kSmall) {
+                if (tid == 0) sh.border = border;
                 __syncthreads();
-                sort_list<THREADS, true>(sh.list, listed);
-                constexpr int M = kList / THREADS;
-                u64 w[M], sum = 0, total;
-#pragma unroll
-                for (int i = 0; i < M; ++i) {
-                    const int at = tid * M + i;
-                    w[i] = at < listed ? by_weight ? weight(logit_of(sh.list[at])) : 1 : 0;
-                    sum += w[i];
-                }
-                if (tid == 0) sh.border = listed ? sh.list[listed - 1] : border;
-                u64 upto = block_scan64<THREADS>(sum, sh, total) - sum;
-#pragma unroll
-                for (int i = 0; i < M; ++i) {
-                    if (upto < want && upto + w[i] >= want) sh.border = sh.list[tid * M + i];
-                    upto += w[i];
+                if (tid < some) {
+                    const u64 o = sh.small[tid], w = sh.small_w[tid];
+                    u64 before = 0;
+                    for (int j = 0; j < some; ++j) before += sh.small[j] > o ? sh.small_w[j] : 0;
+                    if (before < want && before + w >= want) { sh.border = o; sh.found_w = w; sh.word = (int)(uint32_t)~o; }
                 }
                 __syncthreads();
-                border = sh.border;
-                return;
+                if (!by_id) border = uniform(sh.border);
+                break;
             }
-            // More words than can be sorted, most of them alike: a histogram over what tells them apart, keys first, then ids.
-            for (int i = tid; i < kBins; i += THREADS) { sh.count[i] = 0; sh.weight[i] = 0; }
+            // More words than are compared one by one: a histogram over the orders that there are.
+            for (int i = tid; i < kBins; i += THREADS) sh.weight[i] = 0;
+            for (int m = 1; m < 64; m <<= 1) {
+                const u64 l = __shfl_xor(least_o, m), h = __shfl_xor(most_o, m);
+                least_o = l < least_o ? l : least_o;
+                most_o = h > most_o ? h : most_o;
+            }
+            if (lane == 0) { sh.low64[wave] = least_o; sh.high64[wave] = most_o; }
             __syncthreads();
-            const bool by_key = low < high;
-            const uint32_t span = by_key ? high - low : min(id_high, (uint32_t)vectors * E - 1) - id_low;
+            low = ~0ull;
+            high = 0;
+            for (int w = 0; w < WAVES; ++w) {
+                low = sh.low64[w] < low ? sh.low64[w] : low;
+                high = sh.high64[w] > high ? sh.high64[w] : high;
+            }
+            low = uniform(low);
+            high = uniform(high);
             int shift = 0;
-            while (span >> shift >= (uint32_t)kBins) ++shift;
-            each([&](float z, uint32_t id) {
-                if (!inside(z, id)) return;
-                const int at = by_key ? (int)((high - key_of(z + 0.f)) >> shift) : (int)((id - id_low) >> shift);
-                if (by_weight) atomicAdd(&sh.weight[at], weight(z));
+            while ((high - low) >> shift >= (u64)kBins) ++shift;
+            over([&](bool is, float z, uint32_t id) {
+                if (!inside(is, z, id)) return;
+                const int at = (int)((high - order(z, id)) >> shift);
+                if (by_weight) atomicAdd(&sh.weight[at], weigh(z));
                 else atomicAdd(&sh.count[at], 1);
             });
             __syncthreads();
             find_bin(by_weight, want);
-            const uint32_t at = (uint32_t)sh.bin << shift, more = (1u << shift) - 1;
             want = sh.want;
-            if (by_key) {
-                high -= at;
-                low = high - low > more ? high - more : low;
-            } else {
-                id_low += at;
-                id_high = min(id_high, id_low + more);
-            }
+            high -= (u64)sh.bin << shift;
+            const u64 more = (1ull << shift) - 1;
+            if (high - low > more) low = high - more;
         }
-    };
-    if (few) {
-        each([&](float z, uint32_t id) { if (z > -INFINITY) atomicAdd(&sh.count[bin_of(z)], 1); });
-        __syncthreads();
-        cut(false, (u64)k);
-        __syncthreads();
-        for (int i = tid; i < kBins; i += THREADS) sh.weight[i] = 0;
-        __syncthreads();
     }
-    if (p < 1.f) {
-        u64 sum = 0, total;
-        each([&](float z, uint32_t id) {
-            if (!kept(z, id)) return;
-            const u64 w = weight(z);
-            if (w == 0) return;
-            sum += w;
-            atomicAdd(&sh.weight[bin_of(z)], w);
-        });
-        block_scan64<THREADS>(sum, sh, total);
-        const u64 want = p > 0.f ? (u64)ceil((double)p * (double)total) : 1;
-        cut(true, want > 0 ? want : 1);
-    }
-    // The draw: sums of waves, of its vectors for the wave that has it, of its lanes, of the lane's words.
-    u64 sum = 0, total;
-    each([&](float z, uint32_t id) {
-        if (!kept(z, id)) return;
-        const u64 w = weight(z);
-        sum += w >= least ? w : 0;
-    });
-    const u64 upto_thread = block_scan64<THREADS>(sum, sh, total);
-    const u64 upto_wave = __shfl(upto_thread, 63), in_wave = wave_sum64(sum);
-    const u64 target = (u64)floor((double)u * (double)total);
-    u64 before = upto_wave - in_wave;
-    if (before <= target && target < upto_wave) {
-        bool done = false;
-        each_vector([&](int r, u32x4 x) {
-            if (done) return;
-            u64 w[E], s = 0;
+    if (!in_list) {
+        // The draw among all words: sums of threads, of the vectors of the wave that has it, of its lanes, of the lane's words.
+        // (of words of a weight of `least` at least; a hundredth of a factor of two is left for the rounding of logarithm and bound)
+        float floor_z = border ? logit_of(border) : -INFINITY;
+        if (least) floor_z = fmaxf(floor_z, (float)(weight.top + ((double)log2f(fminf(mp, 1.f)) - 0.01) / weight.per) - 1e-6f * fabsf(top));
+        floor_z = uniform(floor_z);
+        auto weigh = [&](u32x4 x, int r, u64 (&w)[E]) {
+            u64 s = 0;
+            float high = O::get(x, 0);
 #pragma unroll
-            for (int j = 0; j < E; ++j) {
-                const float z = O::get(x, j);
-                w[j] = kept(z, (uint32_t)((first + r * 64) * E + j)) ? weight(z) : 0;
-                if (w[j] < least) w[j] = 0;
-                s += w[j];
-            }
-            const u64 upto = before + wave_scan64(s, lane), all = __shfl(upto, 63);
-            if (all > target) {
-                u64 at = upto - s;
-                if (at <= target && target < upto) {
+            for (int j = 1; j < E; ++j) high = fmaxf(high, O::get(x, j));
 #pragma unroll
-                    for (int j = 0; j < E; ++j) {
-                        if (at <= target && target < at + w[j]) { sh.word = (first + r * 64) * E + j; sh.found_w = w[j]; }
-                        at += w[j];
+            for (int j = 0; j < E; ++j) w[j] = 0;
+            if (!__any(high >= floor_z && high > -INFINITY)) return s;
+#pragma unroll
+            for (int j = 0; j < E; ++j) w[j] = weight(O::get(x, j));
+            if (border)
+#pragma unroll
+                for (int j = 0; j < E; ++j)
+                    if (place(O::get(x, j), (uint32_t)((first + r * 64) * E + j)) < border) w[j] = 0;
+            if (least)
+#pragma unroll
+                for (int j = 0; j < E; ++j)
+                    if (w[j] < least) w[j] = 0;
+#pragma unroll
+            for (int j = 0; j < E; ++j) s += w[j];
+            return s;
+        };
+        u64 sum = 0, w[E];
+        each_vector([&](int r, u32x4 x) { sum += weigh(x, r, w); });
+        const u64 upto_thread = block_scan64<THREADS>(sum, sh, total), upto_wave = last_lane(upto_thread), in_wave = last_lane(wave_scan64(sum));
+        const u64 target = uniform((u64)floor((double)u * (double)total));
+        u64 before = upto_wave - in_wave;
+        if (before <= target && target < upto_wave) {
+            bool done = false;
+            each_vector([&](int r, u32x4 x) {
+                if (done) return;
+                const u64 s = weigh(x, r, w), upto = before + wave_scan64(s), all = last_lane(upto);
+                if (all > target) {
+                    u64 at = upto - s;
+                    if (at <= target && target < upto) {
+#pragma unroll
+                        for (int j = 0; j < E; ++j) {
+                            if (at <= target && target < at + w[j]) { sh.word = (first + r * 64) * E + j; sh.found_w = w[j]; }
+                            at += w[j];
+                        }
                     }
+                    done = true;
                 }
-                done = true;
-            }
-            before = all;
-        });
+                before = all;
+            });
+        }
+        __syncthreads();
     }
-    __syncthreads();
-    finish(sh.word, sh.found_w, total);
+    if (tid == 0) {
+        a.word[n] = sh.word;
+        if (a.logprob) a.logprob[n] = (float)log((double)sh.found_w / (double)total);
+    }
 }
 
 }  // namespace
