@@ -1,8 +1,12 @@
 // The next word of every row of logits by a given uniform number, with temperature, top-k, top-p and min-p.
 //
 // Words in the order of falling logits, equal ones by rising id, make every limit a prefix: top-k a count, top-p a weight, min-p a
-// least weight.  A prefix is a key (the logit's order-preserving bits) and how many words of that very key belong to it.  Weights are
-// integers, so that sums do not depend on their order.
+// least weight; the draw is a prefix too, in the order of the ids.  Weights are whole numbers (fixed point), so that sums depend neither on
+// their order nor on how a row is cut.  A prefix is found by a histogram over bins that follow the order, the bin in which what is
+// wanted is reached, and the words of that bin, some tens, each compared with each.
+//
+// A row that fits the registers of one workgroup is read once.  Longer ones are cut into segments of that size for four small workgroups each,
+// and take four launches: maxima, histograms, the words of the deciding bin, the draw.
 #include "device_utils.h"
 #include "ops.h"
 
@@ -10,19 +14,23 @@ namespace rnnlm {
 
 namespace {
 
-constexpr int kThreads = 1024;
 typedef unsigned long long u64;
+typedef u32x4 u32x4_any __attribute__((aligned(2)));          // rows may start at any element
+typedef uint32_t u32x16 __attribute__((ext_vector_type(16)));
+typedef uint32_t u32x32 __attribute__((ext_vector_type(32)));
 
-__device__ __forceinline__ float logit(const void *p, long long i, bool bf16) {
-    const float z = bf16 ? bf16_to_f32(static_cast<const uint16_t *>(p)[i]) : static_cast<const float *>(p)[i];
-    return z + 0.f;                                        // -0 is +0
-}
-// Rises with the number: negative numbers have all bits turned, others the sign.
+// ---- order and weight of a word
+
+// Rises with the number: negative numbers have all bits turned, others the sign.  -0 is +0.
 __device__ __forceinline__ uint32_t key_of(float z) {
-    const uint32_t b = __float_as_uint(z);
+    const uint32_t b = __float_as_uint(z + 0.f);
     return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
 }
 __device__ __forceinline__ float of_key(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k); }
+// Falls from word to word: larger logits first, equal ones by rising id.
+__device__ __forceinline__ u64 place(float z, uint32_t id) { return (u64)key_of(z) << 32 | (uint32_t)~id; }
+__device__ __forceinline__ float logit_of(u64 place) { return of_key((uint32_t)(place >> 32)); }
+__device__ __forceinline__ uint32_t id_of(u64 place) { return ~(uint32_t)place; }
 
 // Values that all lanes share, in scalar registers.
 __device__ __forceinline__ uint32_t uniform(uint32_t x) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)x); }
@@ -54,169 +62,26 @@ __device__ __forceinline__ u64 fixed_exp2(double y, int bits) {
     return (u64)__double_as_longlong(ldexp(q, (int)n + bits) + 0x1p52) - 0x4330000000000000ull;
 }
 
-struct Weight {
-    double top, per;       // the row's maximum; log2(e) / temperature
-    int bits;
-    __device__ u64 operator()(float z) const {
-        if (top == (double)INFINITY) return z == INFINITY ? 1ull << bits : 0;
-        return fixed_exp2(((double)z - top) * per, bits);
-    }
-    __device__ u64 one() const { return 1ull << bits; }
-};
+// ---- sums over a wave and a workgroup
 
-__device__ __forceinline__ u64 wave_sum64(u64 v) {
-#pragma unroll
-    for (int m = 32; m; m >>= 1) v += __shfl_xor(v, m);
-    return v;
+template <int CTRL, int ROWS>
+__device__ __forceinline__ u64 moved(u64 v) {
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)v, CTRL, ROWS, 0xF, false);
+    const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(v >> 32), CTRL, ROWS, 0xF, false);
+    return (u64)hi << 32 | lo;
 }
-
-// The plain form: a workgroup per row, every pass over the row in memory, eight bits of the key at a time.
-__global__ __launch_bounds__(kThreads) void sample_plain_kernel(SampleArgs a, int bits) {
-    __shared__ u64 hist_w[256], wave_w[16];
-    __shared__ int hist_c[256];
-    __shared__ float wave_f[16];
-    __shared__ int wave_c[17];
-    __shared__ u64 s_total, s_w;
-    __shared__ long long s_c;
-    __shared__ uint32_t s_prefix;
-    __shared__ int s_word;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, V = a.V;
-    for (int n = blockIdx.x; n < a.N; n += gridDim.x) {
-        const long long base = n * a.ld;
-        const float T = a.temperature ? a.temperature[n] : 1.f, p = a.top_p ? a.top_p[n] : 1.f, mp = a.min_p ? a.min_p[n] : 0.f, u = a.u[n];
-        const int k = a.top_k ? a.top_k[n] : 0;
-        float top = -INFINITY;
-        bool nan = false;
-        for (int i = tid; i < V; i += kThreads) {
-            const float z = logit(a.logits, base + i, a.bf16);
-            nan |= z != z;
-            top = fmaxf(top, z);
-        }
-        top = wave_max(top);
-        const bool bad_row = __syncthreads_or(nan);
-        if (lane == 0) wave_f[wave] = top;
-        __syncthreads();
-        for (int w = 0; w < 16; ++w) top = fmaxf(top, wave_f[w]);
-        const bool bad = bad_row || top == -INFINITY || !(T >= 0.f) || T == INFINITY || !(u >= 0.f && u < 1.f) || p != p || mp != mp;
-        const Weight weight{(double)top, T > 0.f ? 1.4426950408889634 / (double)T : 0.0, bits};
-        // A prefix: words of a key above t, and the first m of key t (V: all of them).
-        uint32_t t = 0;
-        long long m = V;
-        u64 total = 0;
-        // The shortest prefix of the present one with `count` words (by_weight false) or a weight of `count` at least.
-        auto cut = [&](bool by_weight, u64 want) {
-            uint32_t prefix = 0;
-            for (int shift = 24; shift >= 0; shift -= 8) {
-                __syncthreads();
-                if (tid < 256) { hist_w[tid] = 0; hist_c[tid] = 0; }
-                __syncthreads();
-                for (int i = tid; i < V; i += kThreads) {
-                    const float z = logit(a.logits, base + i, a.bf16);
-                    const uint32_t key = key_of(z);
-                    if (shift < 24 && (key >> (shift + 8)) != prefix) continue;
-                    if (key < t) continue;
-                    atomicAdd(&hist_c[(key >> shift) & 255], 1);
-                    if (by_weight) atomicAdd(&hist_w[(key >> shift) & 255], weight(z));
-                }
-                __syncthreads();
-                if (tid == 0) {
-                    int b = 255;
-                    for (; b > 0; --b) {
-                        const uint32_t lowest = ((prefix << 8 | (uint32_t)b) << shift);
-                        u64 have = by_weight ? hist_w[b] : (u64)hist_c[b];
-                        // the last key of the present prefix counts no more than m words
-                        if (by_weight && shift == 0 && lowest == t && hist_c[b] > m) have = (u64)m * weight(of_key(t));
-                        if (have >= want) break;
-                        want -= have;
-                    }
-                    s_prefix = prefix << 8 | (uint32_t)b;
-                    s_w = want;
-                }
-                __syncthreads();
-                prefix = s_prefix;
-                want = s_w;
-            }
-            const bool same = prefix == t;
-            t = prefix;
-            const u64 w = by_weight ? weight(of_key(t)) : 1;
-            u64 many = w ? (want + w - 1) / w : (u64)V;
-            if (many < 1) many = 1;
-            if (same && (u64)m < many) many = (u64)m;
-            m = (long long)many;
-        };
-        const u64 least = mp > 0.f ? (u64)ceil((double)fminf(mp, 1.f) * (double)weight.one()) : 0;
-        // tie ranks: words of key t are numbered by id
-        auto sum_kept = [&](bool find, u64 target, u64 floor_w) {
-            __syncthreads();
-            if (tid == 0) { s_total = 0; s_c = 0; s_word = -1; }
-            __syncthreads();
-            for (int i0 = 0; i0 < V; i0 += kThreads) {
-                const int i = i0 + tid;
-                const float z = i < V ? logit(a.logits, base + i, a.bf16) : -INFINITY;
-                const uint32_t key = key_of(z);
-                const bool tie = i < V && key == t;
-                const u64 ties = __ballot(tie);
-                if (lane == 0) wave_c[wave] = __popcll(ties);
-                __syncthreads();
-                long long rank = s_c + __popcll(ties & ((1ull << lane) - 1));
-                int all = 0;
-                for (int w = 0; w < 16; ++w) { if (w < wave) rank += wave_c[w]; all += wave_c[w]; }
-                u64 w = 0;
-                if (i < V && (key > t || (tie && rank < m))) { w = weight(z); if (w < floor_w) w = 0; }
-                const u64 ws = wave_sum64(w);
-                if (lane == 0) wave_w[wave] = ws;
-                __syncthreads();
-                u64 before = s_total, sum = 0;
-                for (int q = 0; q < 16; ++q) { if (q < wave) before += wave_w[q]; sum += wave_w[q]; }
-                if (find && before <= target && before + ws > target) {      // this wave has it
-                    u64 upto = w;
-#pragma unroll
-                    for (int s = 1; s < 64; s <<= 1) { const u64 o = __shfl_up(upto, s); if (lane >= s) upto += o; }
-                    const u64 hit = __ballot(before + upto > target);
-                    if (lane == __ffsll((long long)hit) - 1) { s_word = i; s_w = w; }
-                }
-                __syncthreads();
-                if (tid == 0) { s_total += sum; s_c += all; }
-                __syncthreads();
-                if (find && s_word >= 0) break;
-            }
-            total = s_total;
-            __syncthreads();
-        };
-        if (bad) {
-            if (tid == 0) { a.word[n] = -1; if (a.logprob) a.logprob[n] = quiet_nan(); }
-            continue;
-        }
-        if (T == 0.f) {
-            __syncthreads();
-            if (tid == 0) s_word = 0x7FFFFFFF;
-            __syncthreads();
-            for (int i = tid; i < V; i += kThreads)
-                if (logit(a.logits, base + i, a.bf16) == top) atomicMin(&s_word, i);
-            __syncthreads();
-            if (tid == 0) { a.word[n] = s_word; if (a.logprob) a.logprob[n] = 0.f; }
-            __syncthreads();
-            continue;
-        }
-        if (k > 0 && k < V) cut(false, (u64)k);
-        if (p < 1.f) {
-            sum_kept(false, 0, 0);
-            const u64 want = p > 0.f ? (u64)ceil((double)p * (double)total) : 1;
-            cut(true, want > 0 ? want : 1);
-        }
-        sum_kept(false, 0, least);
-        const u64 whole = total;
-        sum_kept(true, (u64)floor((double)u * (double)whole), least);
-        if (tid == 0) {
-            a.word[n] = s_word;
-            if (a.logprob) a.logprob[n] = (float)log((double)s_w / (double)whole);
-        }
-        __syncthreads();
-    }
+// Inclusive prefix sums in registers, as wave_inclusive_scan.
+__device__ __forceinline__ u64 wave_scan64(u64 v) {
+    v += moved<0x111, 0xF>(v);
+    v += moved<0x112, 0xF>(v);
+    v += moved<0x114, 0xF>(v);
+    v += moved<0x118, 0xF>(v);
+    v += moved<0x142, 0xA>(v);
+    return v + moved<0x143, 0xC>(v);
 }
-
-
-// ---- A row in the registers of one workgroup
+__device__ __forceinline__ u64 of_lane(u64 v, int lane) {
+    return (u64)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(v >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, lane);
+}
 
 // Bins of the distance to the row's maximum, over the kOctaves factors of two in which a weight is not nothing; words that can be listed;
 // words that are put in order by comparing each with each.
@@ -224,15 +89,104 @@ constexpr int kOctaves = 52, kSmall = 256;
 constexpr int bins_of(int threads) { return threads > 256 ? 4096 : 1024; }
 constexpr int list_of(int threads) { return threads > 256 ? 2048 : 512; }
 
-typedef u32x4 u32x4_any __attribute__((aligned(2)));
-typedef uint32_t u32x16 __attribute__((ext_vector_type(16)));
-typedef uint32_t u32x32 __attribute__((ext_vector_type(32)));
+template <int BINS, int LIST>
+struct Shared {
+    union {                                                   // histogram
+        u64 weight[BINS];
+        int count[BINS];
+    };
+    u64 list[LIST];
+    u64 small[kSmall], small_w[kSmall];
+    u64 wave64[16], low64[16], high64[16];
+    float wavef[16];
+    u64 want, found_w, border;
+    int bin, n, word;
+};
+
+// Inclusive over the threads.
+template <int THREADS, typename S>
+__device__ __forceinline__ u64 block_scan64(u64 v, S &sh, u64 &total) {
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    v = wave_scan64(v);
+    __syncthreads();
+    if (lane == 63) sh.wave64[wave] = v;
+    __syncthreads();
+    const u64 all = wave_scan64(lane < THREADS / 64 ? sh.wave64[lane] : 0);
+    total = of_lane(all, 63);
+    return v + (wave > 0 ? of_lane(all, wave - 1) : 0);
+}
+template <int THREADS, typename S>
+__device__ __forceinline__ float block_max(float v, S &sh) {
+    const int lane = threadIdx.x & 63;
+    v = wave_max(v);
+    __syncthreads();
+    if (lane == 0) sh.wavef[threadIdx.x >> 6] = v;
+    __syncthreads();
+    return uniform(wave_max(lane < THREADS / 64 ? sh.wavef[lane] : -INFINITY));
+}
+
+// ---- a row
+
+struct Limits {
+    float T, p, mp, u;
+    int k;
+    __device__ Limits(const SampleArgs &a, int n)
+        : T(a.temperature ? a.temperature[n] : 1.f), p(a.top_p ? a.top_p[n] : 1.f), mp(a.min_p ? a.min_p[n] : 0.f), u(a.u[n]), k(a.top_k ? a.top_k[n] : 0) {}
+    __device__ bool bad() const { return !(T >= 0.f) || T == INFINITY || !(u >= 0.f && u < 1.f) || p != p || mp != mp; }
+    __device__ bool few(int V) const { return k > 0 && k < V; }
+    __device__ bool part() const { return p < 1.f; }
+    __device__ u64 want_p(u64 total) const {
+        const u64 w = p > 0.f ? (u64)ceil((double)p * (double)total) : 1;
+        return w > 0 ? w : 1;
+    }
+    __device__ u64 target(u64 total) const { return uniform((u64)floor((double)u * (double)total)); }
+};
+
+// Weights and bins of a row whose maximum is known.
+struct Scale {
+    double high, per;                                         // the maximum; log2(e) / temperature
+    float top, bin_scale;
+    int bits, last_bin;
+    bool alike;                                               // a maximum of +infinity: those words are 0 here, all others -infinity
+    u64 least;                                                // min_p's weight
+    __device__ Scale(const Limits &l, float maximum, int bits, int bins) : bits(bits), last_bin(bins - 1) {
+        alike = maximum == INFINITY;
+        top = alike ? 0.f : maximum;
+        high = uniform((double)top);
+        per = uniform(1.4426950408889634 / (double)l.T);
+        bin_scale = uniform(fminf((float)(per * ((double)bins / kOctaves)), 3.4e38f));
+        least = l.mp > 0.f ? uniform((u64)ceil((double)fminf(l.mp, 1.f) * (double)(1ull << bits))) : 0;
+    }
+    __device__ __forceinline__ float seen(float z) const { return !alike ? z : z == INFINITY ? 0.f : -INFINITY; }
+    __device__ __forceinline__ u64 weight(float z) const { return fixed_exp2(((double)z - high) * per, bits); }
+    // rises as z falls; what is in the last one weighs nothing
+    __device__ __forceinline__ int bin_of(float z) const {
+        const float x = (top - z) * bin_scale;
+        return x < (float)last_bin ? (int)x : last_bin;
+    }
+};
+
+template <typename Z> struct Row;
+template <> struct Row<float> {
+    static constexpr int E = 4;
+    static constexpr uint32_t kNothing = 0xFF800000u;
+    static __device__ __forceinline__ float get(u32x4 v, int i) { return __uint_as_float(v[i]); }
+    static __device__ __forceinline__ float one(const float *p) { return *p; }
+    static __device__ __forceinline__ uint32_t pack(const float (&z)[4], int i) { return __float_as_uint(z[i]); }
+};
+template <> struct Row<uint16_t> {
+    static constexpr int E = 8;
+    static constexpr uint32_t kNothing = 0xFF80FF80u;
+    static __device__ __forceinline__ float get(u32x4 v, int i) { return __uint_as_float(i & 1 ? v[i >> 1] & 0xFFFF0000u : v[i >> 1] << 16); }
+    static __device__ __forceinline__ float one(const uint16_t *p) { return bf16_to_f32(*p); }
+    static __device__ __forceinline__ uint32_t pack(const float (&z)[8], int i) { return __float_as_uint(z[2 * i]) >> 16 | (__float_as_uint(z[2 * i + 1]) & 0xFFFF0000u); }   // (bfloat16 values)
+};
+
 // R vectors of 16 bytes that a loop reads by a counter: code that runs once for a row and is written out for every one of its vectors is not
-// executed but fetched (a third of a megabyte of it took 345 us where this takes a tenth).
+// executed but fetched (256 rows of 65536: 314 KB of code 345 us, 50 KB 119).
 template <int R> struct Vectors;
 template <> struct Vectors<4> {
     u32x16 x;
-    __device__ __forceinline__ u32x4 get(int r) const { return u32x4{x[4 * r], x[4 * r + 1], x[4 * r + 2], x[4 * r + 3]}; }
     __device__ __forceinline__ void set(int r, u32x4 v) {
 #pragma unroll
         for (int q = 0; q < 4; ++q) x[4 * r + q] = v[q];
@@ -240,7 +194,7 @@ template <> struct Vectors<4> {
     // f(r, vector) for r below `used`
     template <typename F> __device__ __forceinline__ void each(int used, F f) const {
 #pragma unroll 1
-        for (int r = 0; r < 4 && r < used; ++r) f(r, get(r));
+        for (int r = 0; r < 4 && r < used; ++r) f(r, u32x4{x[4 * r], x[4 * r + 1], x[4 * r + 2], x[4 * r + 3]});
     }
 };
 template <> struct Vectors<16> {
@@ -260,191 +214,147 @@ template <> struct Vectors<16> {
     }
 };
 
-template <typename Z> struct RowOf;
-template <> struct RowOf<float> {
-    static constexpr int E = 4;
-    static constexpr uint32_t kNothing = 0xFF800000u;
-    static __device__ __forceinline__ float get(u32x4 v, int i) { return __uint_as_float(v[i]); }
-    static __device__ __forceinline__ float one(const float *p) { return *p; }
-    static __device__ __forceinline__ uint32_t pack(const float (&z)[4], int i) { return __float_as_uint(z[i]); }
-};
-template <> struct RowOf<uint16_t> {
-    static constexpr int E = 8;
-    static constexpr uint32_t kNothing = 0xFF80FF80u;
-    static __device__ __forceinline__ float get(u32x4 v, int i) { return __uint_as_float(i & 1 ? v[i >> 1] & 0xFFFF0000u : v[i >> 1] << 16); }
-    static __device__ __forceinline__ float one(const uint16_t *p) { return bf16_to_f32(*p); }
-    static __device__ __forceinline__ uint32_t pack(const float (&z)[8], int i) { return __float_as_uint(z[2 * i]) >> 16 | (__float_as_uint(z[2 * i + 1]) & 0xFFFF0000u); }   // (bfloat16 values)
-};
-
-// Inclusive prefix sums over the wave in registers, as wave_inclusive_scan.
-template <int CTRL, int ROWS>
-__device__ __forceinline__ u64 moved(u64 v) {
-    const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)v, CTRL, ROWS, 0xF, false);
-    const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(v >> 32), CTRL, ROWS, 0xF, false);
-    return (u64)hi << 32 | lo;
-}
-__device__ __forceinline__ u64 wave_scan64(u64 v) {
-    v += moved<0x111, 0xF>(v);
-    v += moved<0x112, 0xF>(v);
-    v += moved<0x114, 0xF>(v);
-    v += moved<0x118, 0xF>(v);
-    v += moved<0x142, 0xA>(v);
-    return v + moved<0x143, 0xC>(v);
-}
-__device__ __forceinline__ u64 last_lane(u64 v) {
-    return (u64)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(v >> 32), 63) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, 63);
-}
-// Order of the words: larger logits first, equal ones by rising id.
-__device__ __forceinline__ u64 place(float z, uint32_t id) { return (u64)key_of(z + 0.f) << 32 | (uint32_t)~id; }
-__device__ __forceinline__ float logit_of(u64 place) { return of_key((uint32_t)(place >> 32)); }
-
-template <int THREADS>
-struct Shared {
-    union {                                  // histogram
-        u64 weight[bins_of(THREADS)];
-        int count[bins_of(THREADS)];
-    };
-    u64 list[list_of(THREADS)];
-    u64 small[kSmall], small_w[kSmall];
-    u64 wave64[16], low64[16], high64[16];
-    float wavef[16];
-    u64 want, found_w, border;
-    int bin, n, word;
-};
-
-// Inclusive over the threads.
-template <int THREADS>
-__device__ __forceinline__ u64 block_scan64(u64 v, Shared<THREADS> &sh, u64 &total) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    v = wave_scan64(v);
-    __syncthreads();
-    if (lane == 63) sh.wave64[wave] = v;
-    __syncthreads();
-    const u64 all = wave_scan64(lane < THREADS / 64 ? sh.wave64[lane] : 0);
-    total = last_lane(all);
-    const int before = __builtin_amdgcn_readfirstlane(wave) - 1;
-    const uint32_t lo = before < 0 ? 0 : (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)all, before);
-    const uint32_t hi = before < 0 ? 0 : (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(all >> 32), before);
-    return v + ((u64)hi << 32 | lo);
-}
-
+// n words from `row` on in the registers of a workgroup; elements behind them are -infinity.  A wave's vectors lie behind each other, so
+// that ids rise with wave, vector, lane, element.
 template <typename Z, int THREADS, int R>
-__global__ __launch_bounds__(THREADS, 4) void sample_row_kernel(SampleArgs a, int bits) {
-    typedef RowOf<Z> O;
-    constexpr int E = O::E, WAVES = THREADS / 64, kBins = bins_of(THREADS), kList = list_of(THREADS), kPerThread = kBins / THREADS;
-    constexpr float kBinsPerOctave = (float)kBins / kOctaves;
-    __shared__ Shared<THREADS> sh;
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = blockIdx.x, V = a.V;
-    const Z *row = static_cast<const Z *>(a.logits) + n * a.ld;
-    const float T = a.temperature ? a.temperature[n] : 1.f, p = a.top_p ? a.top_p[n] : 1.f, mp = a.min_p ? a.min_p[n] : 0.f, u = a.u[n];
-    const int k = a.top_k ? a.top_k[n] : 0;
-    // a wave's vectors lie behind each other: vector (wave * used + r) * 64 + lane, so that words rise with wave, r, lane, element
-    const int vectors = (V + E - 1) / E, used = (vectors + 64 * WAVES - 1) / (64 * WAVES), first = wave * used * 64 + lane;
-    u32x4 loaded[R];
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-        loaded[r] = u32x4{O::kNothing, O::kNothing, O::kNothing, O::kNothing};
-        const int i = first + r * 64;
-        if (r < used && (i + 1) * E <= V) loaded[r] = *reinterpret_cast<const u32x4_any *>(reinterpret_cast<const char *>(row) + (uint32_t)i * 16u);
-    }
-    if (V % E) {                                              // the last vector, element by element
-        const int r_last = (vectors - 1 - first) / 64;
-        if (vectors - 1 == first + r_last * 64 && r_last < used && vectors - 1 >= first) {
-            float z[E];
-#pragma unroll
-            for (int j = 0; j < E; ++j) z[j] = (vectors - 1) * E + j < V ? O::one(row + (vectors - 1) * E + j) : -INFINITY;
-            u32x4 x;
-#pragma unroll
-            for (int q = 0; q < 4; ++q) x[q] = O::pack(z, q);
-#pragma unroll
-            for (int r = 0; r < R; ++r)
-                if (r == r_last) loaded[r] = x;
-        }
-    }
+struct Words {
+    typedef Z Type;
+    static constexpr int E = Row<Z>::E;
     Vectors<R> v;
+    int used, first;                                          // vectors of a thread; index of its first
+    __device__ __forceinline__ Words(const Z *row, int n) {
+        const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), vectors = (n + E - 1) / E;
+        used = (vectors + THREADS - 1) / THREADS;
+        first = wave * used * 64 + lane;
+        u32x4 loaded[R];
 #pragma unroll
-    for (int r = 0; r < R; ++r) v.set(r, loaded[r]);
-    bool alike = false;                                       // +infinity is 0 from here on, all else -infinity
-    auto each_vector = [&](auto f) {                          // f(r, vector)
+        for (int r = 0; r < R; ++r) {
+            loaded[r] = u32x4{Row<Z>::kNothing, Row<Z>::kNothing, Row<Z>::kNothing, Row<Z>::kNothing};
+            const int i = first + r * 64;
+            if (r < used && (i + 1) * E <= n) loaded[r] = *reinterpret_cast<const u32x4_any *>(reinterpret_cast<const char *>(row) + (uint32_t)i * 16u);
+        }
+        if (n % E) {                                          // the last vector, element by element
+            const int last = vectors - 1, r_last = (last - first) / 64;
+            if (last >= first && last == first + r_last * 64 && r_last < used) {
+                float z[E];
+#pragma unroll
+                for (int j = 0; j < E; ++j) z[j] = last * E + j < n ? Row<Z>::one(row + last * E + j) : -INFINITY;
+                u32x4 x;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) x[q] = Row<Z>::pack(z, q);
+#pragma unroll
+                for (int r = 0; r < R; ++r)
+                    if (r == r_last) loaded[r] = x;
+            }
+        }
+#pragma unroll
+        for (int r = 0; r < R; ++r) v.set(r, loaded[r]);
+    }
+    // f(index of the first element, vector as the scale sees it)
+    template <typename F> __device__ __forceinline__ void each_vector(bool alike, F f) const {
         v.each(used, [&](int r, u32x4 x) {
             if (alike) {
                 float z[E];
 #pragma unroll
-                for (int j = 0; j < E; ++j) z[j] = O::get(x, j) == INFINITY ? 0.f : -INFINITY;
+                for (int j = 0; j < E; ++j) z[j] = Row<Z>::get(x, j) == INFINITY ? 0.f : -INFINITY;
 #pragma unroll
-                for (int q = 0; q < 4; ++q) x[q] = O::pack(z, q);
+                for (int q = 0; q < 4; ++q) x[q] = Row<Z>::pack(z, q);
             }
-            f(r, x);
+            f((first + r * 64) * E, x);
         });
-    };
-    auto each = [&](auto f) {                                 // f(logit, id), ids of a thread rising
-        each_vector([&](int r, u32x4 x) {
+    }
+    // f(logit, index), indices of a thread rising
+    template <typename F> __device__ __forceinline__ void each(bool alike, F f) const {
+        each_vector(alike, [&](int i, u32x4 x) {
 #pragma unroll
-            for (int j = 0; j < E; ++j) f(O::get(x, j), (uint32_t)((first + r * 64) * E + j));
+            for (int j = 0; j < E; ++j) f(Row<Z>::get(x, j), (uint32_t)(i + j));
         });
-    };
-    for (int i = tid; i < kBins; i += THREADS) sh.count[i] = 0;
-    if (tid == 0) sh.n = 0;
-    float mine = -INFINITY;
-    bool nan = false;
-    each([&](float z, uint32_t) { mine = fmaxf(mine, z); nan |= z != z; });
-    float top = wave_max(mine);
-    if (lane == 0) sh.wavef[wave] = top;
-    const bool bad = __syncthreads_or(nan || !(T >= 0.f) || T == INFINITY || !(u >= 0.f && u < 1.f) || p != p || mp != mp);
-    top = uniform(wave_max(lane < WAVES ? sh.wavef[lane] : -INFINITY));
-    if (bad || top == -INFINITY) {
-        if (tid == 0) { a.word[n] = -1; if (a.logprob) a.logprob[n] = quiet_nan(); }
-        return;
     }
-    if (T == 0.f) {
-        if (tid == 0) sh.word = 0x7FFFFFFF;
-        __syncthreads();
-        uint32_t at = 0x7FFFFFFF;
-        if (__any(mine == top)) each([&](float z, uint32_t id) { at = z == top && id < at ? id : at; });
-        if (at != 0x7FFFFFFF) atomicMin(&sh.word, (int)at);
-        __syncthreads();
-        if (tid == 0) { a.word[n] = sh.word; if (a.logprob) a.logprob[n] = 0.f; }
-        return;
+    // This thread's largest logit; NaN where there is one.
+    __device__ __forceinline__ float largest() const {
+        float high = -INFINITY;
+        bool nan = false;
+        each(false, [&](float z, uint32_t) { high = fmaxf(high, z); nan |= z != z; });
+        return nan ? quiet_nan() : high;
     }
-    if (top == INFINITY) {                                    // those words alone, alike
-        alike = true;
-        mine = mine == INFINITY ? 0.f : -INFINITY;
-        top = 0.f;
-    }
-    const Weight weight{uniform((double)top), uniform(1.4426950408889634 / (double)T), bits};
-    const float bin_scale = uniform(fminf((float)(weight.per * kBinsPerOctave), 3.4e38f));
-    auto bin_of = [&](float z) {                              // rises as z falls; what is in the last one weighs nothing
-        const float x = (top - z) * bin_scale;
-        return x < (float)(kBins - 1) ? (int)x : kBins - 1;
-    };
-    const u64 least = mp > 0.f ? uniform((u64)ceil((double)fminf(mp, 1.f) * (double)weight.one())) : 0;
-    // Appends words to a list, `to` of at most `most`; beyond that they are only counted.  M words of a thread at once.
-    auto append = [&](auto take, auto put, int most) {
-        int at = 0;
-        constexpr int M = sizeof(take) / sizeof(bool);
-        u64 who[M];
-        int all = 0;
+};
+
+// Appends words to a list of at most `most`; beyond that they are only counted in `n`.  put(i, to): which of this thread's M words goes where.
+template <int M>
+struct Taken { bool is[M]; };
+template <int M, typename F>
+__device__ __forceinline__ void append(int *n, const Taken<M> &take, int most, F put) {
+    const int lane = threadIdx.x & 63;
+    u64 who[M];
+    int all = 0, at = 0;
 #pragma unroll
-        for (int i = 0; i < M; ++i) { who[i] = __ballot(take.is[i]); all += __popcll(who[i]); }
-        if (all == 0) return;
-        if (lane == 0) at = atomicAdd(&sh.n, all);
-        at = __builtin_amdgcn_readfirstlane(at);
+    for (int i = 0; i < M; ++i) { who[i] = __ballot(take.is[i]); all += __popcll(who[i]); }
+    if (all == 0) return;
+    if (lane == 0) at = atomicAdd(n, all);
+    at = __builtin_amdgcn_readfirstlane(at);
 #pragma unroll
-        for (int i = 0; i < M; ++i) {
-            const int mine_at = at + __popcll(who[i] & ((1ull << lane) - 1));
-            if (take.is[i] && mine_at < most) put(i, mine_at);
-            at += __popcll(who[i]);
-        }
-    };
-    // The bin where `want` of the histogram (counts, or weights) is reached from the front, and what is still wanted of that bin.
-    auto find_bin = [&](bool by_weight, u64 want) {
+    for (int i = 0; i < M; ++i) {
+        const int to = at + __popcll(who[i] & ((1ull << lane) - 1));
+        if (take.is[i] && to < most) put(i, to);
+        at += __popcll(who[i]);
+    }
+}
+
+// ---- the search for a prefix
+
+enum Kind { kCount, kWeight, kDraw };        // top_k: words, by place.  top_p: weight, by place.  The draw: weight of at least `least`, by id.
+
+// `over(f)` calls f(there, logit, id) for the words of a source (registers, a list, memory), the same number of times in all lanes of a wave.
+template <int THREADS, int BINS, int LIST>
+struct Search {
+    static constexpr int kPerThread = BINS / THREADS, WAVES = THREADS / 64;
+    Shared<BINS, LIST> &sh;
+    const Scale &scale;
+    u64 border;                              // place of the last word kept (0: all)
+    uint32_t id_from;                        // ids go to bins from here on
+    int id_shift;
+    __device__ Search(Shared<BINS, LIST> &sh, const Scale &scale, uint32_t from, int n) : sh(sh), scale(scale), border(0), id_from(from), id_shift(0) {
+        while ((n - 1) >> id_shift >= BINS) ++id_shift;
+    }
+    __device__ __forceinline__ bool kept(float z, uint32_t id) const { return z > -INFINITY && place(z, id) >= border; }
+    __device__ __forceinline__ u64 weigh(Kind kind, float z) const {
+        const u64 w = kind == kCount ? 1 : scale.weight(z);
+        return kind == kDraw && w < scale.least ? 0 : w;
+    }
+    __device__ __forceinline__ int bin_at(Kind kind, float z, uint32_t id) const { return kind == kDraw ? (int)((id - id_from) >> id_shift) : scale.bin_of(z); }
+    __device__ __forceinline__ u64 order(Kind kind, float z, uint32_t id) const { return kind == kDraw ? ~(u64)id : place(z, id); }
+    __device__ __forceinline__ void clear() {
+        __syncthreads();
+        for (int i = threadIdx.x; i < BINS; i += THREADS) sh.weight[i] = 0;
+        __syncthreads();
+    }
+    // Histogram of the words kept; returns their weight (nothing of use for counts).
+    template <typename O>
+    __device__ __forceinline__ u64 histogram(Kind kind, O over) {
+        clear();
+        u64 sum = 0, total;
+        if (kind != kCount) over([&](bool is, float z, uint32_t id) {
+            u64 w = scale.weight(z);
+            w = is && kept(z, id) && !(kind == kDraw && w < scale.least) ? w : 0;
+            sum += w;
+            if (w) atomicAdd(&sh.weight[bin_at(kind, z, id)], w);
+        });
+        else over([&](bool is, float z, uint32_t id) {
+            if (is && kept(z, id)) atomicAdd(&sh.count[scale.bin_of(z)], 1);
+        });
+        block_scan64<THREADS>(sum, sh, total);
+        return total;
+    }
+    // The bin where `want` of the histogram is reached from the front (the last one if it is not), and what is still wanted of that bin.
+    __device__ __forceinline__ int find_bin(bool counts, u64 &want) {
+        const int tid = threadIdx.x;
         u64 h[kPerThread], sum = 0, total;
 #pragma unroll
         for (int i = 0; i < kPerThread; ++i) {
-            h[i] = by_weight ? sh.weight[tid * kPerThread + i] : (u64)sh.count[tid * kPerThread + i];
+            h[i] = counts ? (u64)sh.count[tid * kPerThread + i] : sh.weight[tid * kPerThread + i];
             sum += h[i];
         }
-        if (tid == 0) sh.bin = kBins - 1;
+        if (tid == 0) { sh.bin = BINS - 1; sh.want = want; }
         u64 upto = block_scan64<THREADS>(sum, sh, total) - sum;
         if (upto < want && upto + sum >= want) {
 #pragma unroll
@@ -454,83 +364,19 @@ __global__ __launch_bounds__(THREADS, 4) void sample_row_kernel(SampleArgs a, in
             }
         }
         __syncthreads();
-    };
-
-    // Few words kept: they are listed.  The top_k-th largest of the threads' own maxima is no more than the top_k-th largest logit, so whatever
-    // lies in its bin or in front of it is enough.
-    const bool few = k > 0 && k < V;
-    bool in_list = false;
-    int listed = 0;
-    if (few && k <= THREADS / 2) {
-        if (mine > -INFINITY) atomicAdd(&sh.count[bin_of(mine)], 1);
-        __syncthreads();
-        find_bin(false, (u64)k);
-        const int edge = sh.bin;
-        if (edge < kBins - 1) {
-            each_vector([&](int r, u32x4 x) {
-                struct { bool is[E]; } take;
-#pragma unroll
-                for (int j = 0; j < E; ++j) take.is[j] = (top - O::get(x, j)) * bin_scale < (float)(edge + 1);
-                append(take, [&](int j, int to) { sh.list[to] = place(O::get(x, j), (uint32_t)((first + r * 64) * E + j)); }, kList);
-            });
-            __syncthreads();
-            listed = sh.n;
-            in_list = listed <= kList;
-        }
+        want = uniform(sh.want);
+        return __builtin_amdgcn_readfirstlane(sh.bin);
     }
-    auto over = [&](auto f) {                                 // the listed words, or all
-        if (in_list)
-            for (int i = tid; i - tid < listed; i += THREADS) {
-                const u64 w = i < listed ? sh.list[i] : 0;
-                f(i < listed, logit_of(w), (uint32_t)~(uint32_t)w);
-            }
-        else each([&](float z, uint32_t id) { f(id < (uint32_t)V, z, id); });
-    };
-
-    // Limits as the place of the last word kept: top_k, top_p, and of listed words the draw as well, which is the same search in the order of
-    // the ids.  Each by a histogram, the bin in which what is wanted is reached, and that bin's words.
-    u64 border = 0, total = 0;
-    int id_shift = 0;
-    while (V >> id_shift >= kBins) ++id_shift;
-#pragma unroll 1
-    for (int stage = 0; stage < 3; ++stage) {
-        if (stage == 0 ? !few : stage == 1 ? !(p < 1.f) : !in_list) continue;
-        const bool by_weight = stage > 0, by_id = stage == 2;
-        auto weigh = [&](float z) {
-            const u64 w = by_weight ? weight(z) : 1;
-            return by_id && w < least ? 0 : w;
-        };
-        auto bin_at = [&](float z, uint32_t id) { return by_id ? (int)(id >> id_shift) : bin_of(z); };
-        auto order = [&](float z, uint32_t id) { return by_id ? ~(u64)id : place(z, id); };          // falls from word to word
-        auto is_kept = [&](float z, uint32_t id) { return z > -INFINITY && place(z, id) >= border; };
-        __syncthreads();
-        for (int i = tid; i < kBins; i += THREADS) sh.weight[i] = 0;
-        __syncthreads();
-        u64 sum = 0;
-        if (by_weight) over([&](bool is, float z, uint32_t id) {
-            u64 w = weight(z);
-            w = is && is_kept(z, id) && !(by_id && w < least) ? w : 0;
-            sum += w;
-            if (w) atomicAdd(&sh.weight[bin_at(z, id)], w);
-        });
-        else over([&](bool is, float z, uint32_t id) {
-            if (is && is_kept(z, id)) atomicAdd(&sh.count[bin_at(z, id)], 1);
-        });
-        block_scan64<THREADS>(sum, sh, total);
-        u64 want = (u64)k;
-        if (stage == 1) { want = p > 0.f ? (u64)ceil((double)p * (double)total) : 1; if (want < 1) want = 1; }
-        if (stage == 2) want = (u64)floor((double)u * (double)total) + 1;
-        find_bin(by_weight, want);
-        const int bin = sh.bin;
-        if (bin == kBins - 1 && !by_id) continue;             // beyond it nothing has a weight
-        want = sh.want;
+    // Of the words of `bin` the one at which `want` is reached: the new border, or the word drawn (sh.word, sh.found_w).
+    template <typename O>
+    __device__ __forceinline__ void resolve(Kind kind, int bin, u64 want, O over) {
+        const int tid = threadIdx.x, lane = tid & 63;
         u64 low = 0, high = ~0ull;                            // of the orders
-        // (most vectors have no word of one bin)
         auto inside = [&](bool is, float z, uint32_t id) {
-            bool yes = is && bin_at(z, id) == bin;
-            if (!__any(yes)) return false;
-            const u64 o = order(z, id);
-            return yes && is_kept(z, id) && o >= low && o <= high;
+            const bool yes = is && bin_at(kind, z, id) == bin;
+            if (!__any(yes)) return false;                    // (most vectors have no word of one bin)
+            const u64 o = order(kind, z, id);
+            return yes && kept(z, id) && o >= low && o <= high;
         };
         while (true) {
             __syncthreads();
@@ -538,14 +384,14 @@ __global__ __launch_bounds__(THREADS, 4) void sample_row_kernel(SampleArgs a, in
             __syncthreads();
             u64 least_o = ~0ull, most_o = 0;
             over([&](bool is, float z, uint32_t id) {
-                struct { bool is[1]; } take = {{inside(is, z, id)}};
+                const Taken<1> take = {{inside(is, z, id)}};
                 if (!__any(take.is[0])) return;
-                const u64 o = order(z, id);
+                const u64 o = order(kind, z, id);
                 if (take.is[0]) { least_o = o < least_o ? o : least_o; most_o = o > most_o ? o : most_o; }
-                append(take, [&](int, int to) { sh.small[to] = o; sh.small_w[to] = weigh(z); }, kSmall);
+                append(&sh.n, take, kSmall, [&](int, int to) { sh.small[to] = o; sh.small_w[to] = weigh(kind, z); });
             });
             __syncthreads();
-            const int some = sh.n;
+            const int some = __builtin_amdgcn_readfirstlane(sh.n);
             if (some <= kSmall) {
                 if (tid == 0) sh.border = border;
                 __syncthreads();
@@ -553,21 +399,20 @@ __global__ __launch_bounds__(THREADS, 4) void sample_row_kernel(SampleArgs a, in
                     const u64 o = sh.small[tid], w = sh.small_w[tid];
                     u64 before = 0;
                     for (int j = 0; j < some; ++j) before += sh.small[j] > o ? sh.small_w[j] : 0;
-                    if (before < want && before + w >= want) { sh.border = o; sh.found_w = w; sh.word = (int)(uint32_t)~o; }
+                    if (before < want && before + w >= want) { sh.border = o; sh.found_w = w; sh.word = (int)id_of(o); }
                 }
                 __syncthreads();
-                if (!by_id) border = uniform(sh.border);
-                break;
+                if (kind != kDraw) border = uniform(sh.border);
+                return;
             }
             // More words than are compared one by one: a histogram over the orders that there are.
-            for (int i = tid; i < kBins; i += THREADS) sh.weight[i] = 0;
             for (int m = 1; m < 64; m <<= 1) {
                 const u64 l = __shfl_xor(least_o, m), h = __shfl_xor(most_o, m);
                 least_o = l < least_o ? l : least_o;
                 most_o = h > most_o ? h : most_o;
             }
-            if (lane == 0) { sh.low64[wave] = least_o; sh.high64[wave] = most_o; }
-            __syncthreads();
+            if (lane == 0) { sh.low64[tid >> 6] = least_o; sh.high64[tid >> 6] = most_o; }
+            clear();
             low = ~0ull;
             high = 0;
             for (int w = 0; w < WAVES; ++w) {
@@ -577,102 +422,420 @@ __global__ __launch_bounds__(THREADS, 4) void sample_row_kernel(SampleArgs a, in
             low = uniform(low);
             high = uniform(high);
             int shift = 0;
-            while ((high - low) >> shift >= (u64)kBins) ++shift;
+            while ((high - low) >> shift >= (u64)BINS) ++shift;
             over([&](bool is, float z, uint32_t id) {
                 if (!inside(is, z, id)) return;
-                const int at = (int)((high - order(z, id)) >> shift);
-                if (by_weight) atomicAdd(&sh.weight[at], weigh(z));
-                else atomicAdd(&sh.count[at], 1);
+                const int at = (int)((high - order(kind, z, id)) >> shift);
+                if (kind == kCount) atomicAdd(&sh.count[at], 1);
+                else atomicAdd(&sh.weight[at], weigh(kind, z));
             });
             __syncthreads();
-            find_bin(by_weight, want);
-            want = sh.want;
-            high -= (u64)sh.bin << shift;
+            high -= (u64)find_bin(kind == kCount, want) << shift;
             const u64 more = (1ull << shift) - 1;
             if (high - low > more) low = high - more;
         }
     }
-    if (!in_list) {
-        // The draw among all words: sums of threads, of the vectors of the wave that has it, of its lanes, of the lane's words.
-        // (of words of a weight of `least` at least; a hundredth of a factor of two is left for the rounding of logarithm and bound)
-        float floor_z = border ? logit_of(border) : -INFINITY;
-        if (least) floor_z = fmaxf(floor_z, (float)(weight.top + ((double)log2f(fminf(mp, 1.f)) - 0.01) / weight.per) - 1e-6f * fabsf(top));
-        floor_z = uniform(floor_z);
-        auto weigh = [&](u32x4 x, int r, u64 (&w)[E]) {
-            u64 s = 0;
-            float high = O::get(x, 0);
-#pragma unroll
-            for (int j = 1; j < E; ++j) high = fmaxf(high, O::get(x, j));
-#pragma unroll
-            for (int j = 0; j < E; ++j) w[j] = 0;
-            if (!__any(high >= floor_z && high > -INFINITY)) return s;
-#pragma unroll
-            for (int j = 0; j < E; ++j) w[j] = weight(O::get(x, j));
-            if (border)
-#pragma unroll
-                for (int j = 0; j < E; ++j)
-                    if (place(O::get(x, j), (uint32_t)((first + r * 64) * E + j)) < border) w[j] = 0;
-            if (least)
-#pragma unroll
-                for (int j = 0; j < E; ++j)
-                    if (w[j] < least) w[j] = 0;
-#pragma unroll
-            for (int j = 0; j < E; ++j) s += w[j];
-            return s;
-        };
-        u64 sum = 0, w[E];
-        each_vector([&](int r, u32x4 x) { sum += weigh(x, r, w); });
-        const u64 upto_thread = block_scan64<THREADS>(sum, sh, total), upto_wave = last_lane(upto_thread), in_wave = last_lane(wave_scan64(sum));
-        const u64 target = uniform((u64)floor((double)u * (double)total));
-        u64 before = upto_wave - in_wave;
-        if (before <= target && target < upto_wave) {
-            bool done = false;
-            each_vector([&](int r, u32x4 x) {
-                if (done) return;
-                const u64 s = weigh(x, r, w), upto = before + wave_scan64(s), all = last_lane(upto);
-                if (all > target) {
-                    u64 at = upto - s;
-                    if (at <= target && target < upto) {
-#pragma unroll
-                        for (int j = 0; j < E; ++j) {
-                            if (at <= target && target < at + w[j]) { sh.word = (first + r * 64) * E + j; sh.found_w = w[j]; }
-                            at += w[j];
-                        }
-                    }
-                    done = true;
-                }
-                before = all;
-            });
-        }
-        __syncthreads();
+    // One limit, or the draw: the weight of all words it was made of (0 where nothing had to be searched).
+    template <typename O>
+    __device__ __forceinline__ u64 step(Kind kind, const Limits &l, O over) {
+        const u64 total = histogram(kind, over);
+        u64 want = kind == kCount ? (u64)l.k : kind == kWeight ? l.want_p(total) : l.target(total) + 1;
+        const int bin = find_bin(kind == kCount, want);
+        if (bin < BINS - 1 || kind == kDraw) resolve(kind, bin, want, over);      // in the last bin nothing has a weight
+        return total;
     }
-    if (tid == 0) {
-        a.word[n] = sh.word;
-        if (a.logprob) a.logprob[n] = (float)log((double)sh.found_w / (double)total);
+    // All limits and the draw.
+    template <typename O>
+    __device__ __forceinline__ u64 all_steps(const Limits &l, int V, O over) {
+        u64 total = 0;
+#pragma unroll 1
+        for (int kind = kCount; kind <= kDraw; ++kind)
+            if (kind == kCount ? l.few(V) : kind == kWeight ? l.part() : true) total = step((Kind)kind, l, over);
+        return total;
+    }
+};
+
+__device__ __forceinline__ void answer(const SampleArgs &a, int n, int word, float logprob) {
+    if (threadIdx.x == 0) {
+        a.word[n] = word;
+        if (a.logprob) a.logprob[n] = logprob;
+    }
+}
+__device__ __forceinline__ float log_share(u64 w, u64 total) { return (float)log((double)w / (double)total); }
+
+// The draw among n words in registers that `border` keeps, in the order of the ids: sums of threads, of the vectors of the wave that has it, of
+// its lanes, of the lane's words.
+template <int THREADS, typename W, typename S>
+__device__ __forceinline__ u64 draw_from_registers(const W &words, S &sh, const Scale &scale, const Limits &l, u64 border) {
+    constexpr int E = W::E;
+    // no word below it is kept (by min_p: of a weight of `least` at least, with a hundredth of a factor of two for what logarithm and bound are off)
+    float floor_z = border ? logit_of(border) : -INFINITY;
+    if (scale.least) floor_z = fmaxf(floor_z, (float)(scale.high + ((double)log2f(fminf(l.mp, 1.f)) - 0.01) / scale.per) - 1e-6f * fabsf(scale.top));
+    floor_z = uniform(floor_z);
+    u64 w[E];
+    auto weigh = [&](int i, u32x4 x) {
+        u64 s = 0;
+        float high = Row<typename W::Type>::get(x, 0);
+#pragma unroll
+        for (int j = 1; j < E; ++j) high = fmaxf(high, Row<typename W::Type>::get(x, j));
+#pragma unroll
+        for (int j = 0; j < E; ++j) w[j] = 0;
+        if (!__any(high >= floor_z && high > -INFINITY)) return s;
+#pragma unroll
+        for (int j = 0; j < E; ++j) w[j] = scale.weight(Row<typename W::Type>::get(x, j));
+        if (border)
+#pragma unroll
+            for (int j = 0; j < E; ++j)
+                if (place(Row<typename W::Type>::get(x, j), (uint32_t)(i + j)) < border) w[j] = 0;
+        if (scale.least)
+#pragma unroll
+            for (int j = 0; j < E; ++j)
+                if (w[j] < scale.least) w[j] = 0;
+#pragma unroll
+        for (int j = 0; j < E; ++j) s += w[j];
+        return s;
+    };
+    u64 sum = 0, total;
+    words.each_vector(scale.alike, [&](int i, u32x4 x) { sum += weigh(i, x); });
+    const u64 upto_wave = of_lane(block_scan64<THREADS>(sum, sh, total), 63), target = l.target(total);
+    u64 before = upto_wave - of_lane(wave_scan64(sum), 63);
+    if (before <= target && target < upto_wave) {
+        bool done = false;
+        words.each_vector(scale.alike, [&](int i, u32x4 x) {
+            if (done) return;
+            const u64 s = weigh(i, x), upto = before + wave_scan64(s), all = of_lane(upto, 63);
+            if (all > target) {
+                u64 at = upto - s;
+                if (at <= target && target < upto) {
+#pragma unroll
+                    for (int j = 0; j < E; ++j) {
+                        if (at <= target && target < at + w[j]) { sh.word = i + j; sh.found_w = w[j]; }
+                        at += w[j];
+                    }
+                }
+                done = true;
+            }
+            before = all;
+        });
+    }
+    __syncthreads();
+    return total;
+}
+
+// A row in the registers of one workgroup.
+template <typename Z, int THREADS, int R>
+__global__ __launch_bounds__(THREADS, 4) void sample_row_kernel(SampleArgs a, int bits) {
+    constexpr int BINS = bins_of(THREADS), LIST = list_of(THREADS), E = Row<Z>::E;
+    __shared__ Shared<BINS, LIST> sh;
+    const int tid = threadIdx.x, n = blockIdx.x, V = a.V;
+    const Limits l(a, n);
+    const Words<Z, THREADS, R> words(static_cast<const Z *>(a.logits) + n * a.ld, V);
+    for (int i = tid; i < BINS; i += THREADS) sh.count[i] = 0;
+    if (tid == 0) { sh.n = 0; sh.word = 0x7FFFFFFF; }
+    float mine = words.largest();
+    const bool nan = __syncthreads_or(mine != mine);
+    const float maximum = block_max<THREADS>(mine, sh);
+    if (nan || l.bad() || maximum == -INFINITY) { answer(a, n, -1, quiet_nan()); return; }
+    if (l.T == 0.f) {
+        uint32_t at = 0x7FFFFFFF;
+        if (__any(mine == maximum)) words.each(false, [&](float z, uint32_t id) { at = z == maximum && id < at ? id : at; });
+        if (at != 0x7FFFFFFF) atomicMin(&sh.word, (int)at);
+        __syncthreads();
+        answer(a, n, sh.word, 0.f);
+        return;
+    }
+    const Scale scale(l, maximum, bits, BINS);
+    mine = scale.seen(mine);
+    Search<THREADS, BINS, LIST> search(sh, scale, 0, V);
+    // Few words kept: they are listed.  The top_k-th largest of the threads' own maxima is no more than the top_k-th largest logit, so whatever
+    // lies in its bin or in front of it is enough.
+    bool in_list = false;
+    int listed = 0;
+    if (l.few(V) && l.k <= THREADS / 2) {
+        if (mine > -INFINITY) atomicAdd(&sh.count[scale.bin_of(mine)], 1);
+        __syncthreads();
+        u64 want = (u64)l.k;
+        const int edge = search.find_bin(true, want);
+        if (edge < BINS - 1) {
+            words.each_vector(scale.alike, [&](int i, u32x4 x) {
+                Taken<E> take;
+#pragma unroll
+                for (int j = 0; j < E; ++j) take.is[j] = (scale.top - Row<Z>::get(x, j)) * scale.bin_scale < (float)(edge + 1);
+                append(&sh.n, take, LIST, [&](int j, int to) { sh.list[to] = place(Row<Z>::get(x, j), (uint32_t)(i + j)); });
+            });
+            __syncthreads();
+            listed = __builtin_amdgcn_readfirstlane(sh.n);
+            in_list = listed <= LIST;
+        }
+    }
+    auto over = [&](auto f) {
+        if (in_list)
+            for (int i = tid; i - tid < listed; i += THREADS) {
+                const u64 w = i < listed ? sh.list[i] : 0;
+                f(i < listed, logit_of(w), id_of(w));
+            }
+        else words.each(scale.alike, [&](float z, uint32_t id) { f(id < (uint32_t)V, z, id); });
+    };
+    u64 total = 0;
+#pragma unroll 1
+    for (int kind = kCount; kind <= kDraw; ++kind)
+        if (kind == kCount ? l.few(V) : kind == kWeight ? l.part() : in_list) total = search.step((Kind)kind, l, over);
+    if (!in_list) total = draw_from_registers<THREADS>(words, sh, scale, l, search.border);
+    answer(a, n, sh.word, log_share(sh.found_w, total));
+}
+
+// ---- rows in segments
+
+constexpr int kSegThreads = 256, kSegVectors = 16, kLongBins = 4096, kLongList = 8192, kPickThreads = 1024;
+template <typename Z> constexpr int segment_words() { return kSegThreads * kSegVectors * Row<Z>::E; }
+
+// Of one row in the workspace, behind its histogram of kLongBins weights (or counts): the deciding bin and what is wanted of it, the words listed,
+// how many there are, and of every segment its maximum and the weight of its words that are kept for certain.
+struct LongRow {
+    u64 *hist, *list, *sums;
+    u64 *want;
+    int *bin, *listed;
+    float *tops;
+    static __host__ __device__ size_t bytes(int segments) { return (size_t)(kLongBins + kLongList + segments) * 8 + 16 + ((size_t)segments * 4 + 15) / 16 * 16; }
+    __device__ LongRow(void *ws, int n, int segments) {
+        char *p = static_cast<char *>(ws) + n * bytes(segments);
+        hist = reinterpret_cast<u64 *>(p);
+        list = hist + kLongBins;
+        sums = list + kLongList;
+        want = sums + segments;
+        bin = reinterpret_cast<int *>(want + 1);
+        listed = bin + 1;
+        tops = reinterpret_cast<float *>(listed + 1);
+    }
+    // The row's maximum; NaN where there is one.
+    template <int THREADS, typename S>
+    __device__ __forceinline__ float maximum(int segments, S &sh) const {
+        float m = -INFINITY;
+        bool nan = false;
+        for (int i = threadIdx.x; i < segments; i += THREADS) {
+            const float t = tops[i];
+            nan |= t != t;
+            m = fmaxf(m, t);
+        }
+        nan = __syncthreads_or(nan);
+        m = block_max<THREADS>(m, sh);
+        return nan ? quiet_nan() : m;
+    }
+};
+// Of a row with top_k all words that can be kept are listed, and the last launch does the rest, unless they are too many; then, and with top_p alone,
+// the words of the deciding bin.  (Too many with top_p as well: the last launch reads the row itself.)
+__device__ __forceinline__ bool lists_all(const Limits &l, int V) { return l.few(V) && l.k <= kLongList / 2; }
+__device__ __forceinline__ bool lists_bin(const Limits &l, int V) { return l.few(V) ? !lists_all(l, V) && !l.part() : l.part(); }
+
+template <typename Z>
+__global__ __launch_bounds__(kSegThreads) void sample_tops_kernel(SampleArgs a, int segments) {
+    __shared__ Shared<16, 1> sh;
+    const int n = blockIdx.x / segments, s = blockIdx.x % segments, from = s * segment_words<Z>(), len = min(a.V - from, segment_words<Z>());
+    const LongRow r(a.ws, n, segments);
+    const Words<Z, kSegThreads, kSegVectors> words(static_cast<const Z *>(a.logits) + n * a.ld + from, len);
+    for (int i = s * kSegThreads + threadIdx.x; i < kLongBins; i += segments * kSegThreads) r.hist[i] = 0;
+    if (s == 0 && threadIdx.x == 0) *r.listed = 0;
+    const float mine = words.largest();
+    const bool nan = __syncthreads_or(mine != mine);
+    const float top = block_max<kSegThreads>(mine, sh);
+    if (threadIdx.x == 0) r.tops[s] = nan ? quiet_nan() : top;
+}
+
+template <typename Z>
+__global__ __launch_bounds__(kSegThreads) void sample_weigh_kernel(SampleArgs a, int segments, int bits) {
+    __shared__ Shared<kLongBins, 1> sh;
+    const int n = blockIdx.x / segments, s = blockIdx.x % segments, from = s * segment_words<Z>(), len = min(a.V - from, segment_words<Z>());
+    const Limits l(a, n);
+    const LongRow r(a.ws, n, segments);
+    const Words<Z, kSegThreads, kSegVectors> words(static_cast<const Z *>(a.logits) + n * a.ld + from, len);
+    const float maximum = r.maximum<kSegThreads>(segments, sh);
+    if (l.bad() || !(maximum > -INFINITY) || l.T == 0.f) return;
+    const Scale scale(l, maximum, bits, kLongBins);
+    Search<kSegThreads, kLongBins, 1> search(sh, scale, 0, a.V);
+    auto over = [&](auto f) { words.each(scale.alike, [&](float z, uint32_t id) { f(id < (uint32_t)len, z, id); }); };
+    if (!l.few(a.V) && !l.part()) {
+        u64 sum = 0, total;
+        over([&](bool is, float z, uint32_t) { sum += is ? search.weigh(kDraw, z) : 0; });
+        block_scan64<kSegThreads>(sum, sh, total);
+        if (threadIdx.x == 0) r.sums[s] = total;
+        return;
+    }
+    const bool counts = l.few(a.V);
+    search.histogram(counts ? kCount : kWeight, over);
+    for (int i = threadIdx.x; i < kLongBins; i += kSegThreads) {
+        const u64 h = counts ? (u64)sh.count[i] : sh.weight[i];
+        if (h) atomicAdd(&r.hist[i], h);
     }
 }
 
-}  // namespace
-
-size_t sample_workspace_bytes(int N, int V) { return 256; }
-
-namespace {
 template <typename Z>
-hipError_t launch_rows(const SampleArgs &a, int bits, hipStream_t stream) {
-    const int vectors = (a.V + RowOf<Z>::E - 1) / RowOf<Z>::E;
+__global__ __launch_bounds__(kSegThreads) void sample_gather_kernel(SampleArgs a, int segments, int bits) {
+    constexpr int E = Row<Z>::E;
+    __shared__ Shared<kLongBins, 1> sh;
+    const int tid = threadIdx.x, n = blockIdx.x / segments, s = blockIdx.x % segments, from = s * segment_words<Z>(), len = min(a.V - from, segment_words<Z>());
+    const Limits l(a, n);
+    const bool all = lists_all(l, a.V);
+    if (!all && !lists_bin(l, a.V)) return;
+    const LongRow r(a.ws, n, segments);
+    const Words<Z, kSegThreads, kSegVectors> words(static_cast<const Z *>(a.logits) + n * a.ld + from, len);
+    const float maximum = r.maximum<kSegThreads>(segments, sh);
+    if (l.bad() || !(maximum > -INFINITY) || l.T == 0.f) return;
+    const Scale scale(l, maximum, bits, kLongBins);
+    Search<kSegThreads, kLongBins, 1> search(sh, scale, 0, a.V);
+    u64 sum = 0, total;
+    __syncthreads();
+    for (int i = tid; i < kLongBins; i += kSegThreads) {
+        sh.weight[i] = r.hist[i];
+        sum += sh.weight[i];
+    }
+    block_scan64<kSegThreads>(sum, sh, total);
+    u64 want = l.few(a.V) ? (u64)l.k : l.want_p(total);
+    const int bin = search.find_bin(false, want);
+    if (s == 0 && tid == 0) { *r.bin = bin; *r.want = want; }
+    // The words of the bin, or all up to it; a whole wave's words take one number from the row's counter.
+    words.each_vector(scale.alike, [&](int i, u32x4 x) {
+        Taken<E> take;
+        bool any = false;
+#pragma unroll
+        for (int j = 0; j < E; ++j) {
+            const float z = Row<Z>::get(x, j);
+            const int b = scale.bin_of(z);
+            take.is[j] = z > -INFINITY && i + j < len && (all ? b <= bin : b == bin && bin < kLongBins - 1);
+            any |= take.is[j];
+        }
+        if (__any(any)) append(r.listed, take, kLongList, [&](int j, int to) { r.list[to] = place(Row<Z>::get(x, j), (uint32_t)(from + i + j)); });
+    });
+    if (all) return;
+    sum = 0;
+    words.each_vector(scale.alike, [&](int i, u32x4 x) {
+        bool any = false;
+#pragma unroll
+        for (int j = 0; j < E; ++j) any |= scale.bin_of(Row<Z>::get(x, j)) < bin;
+        if (!__any(any)) return;
+#pragma unroll
+        for (int j = 0; j < E; ++j) {
+            const float z = Row<Z>::get(x, j);
+            sum += scale.bin_of(z) < bin ? search.weigh(kDraw, z) : 0;
+        }
+    });
+    block_scan64<kSegThreads>(sum, sh, total);
+    if (tid == 0) r.sums[s] = total;
+}
+
+template <typename Z>
+__global__ __launch_bounds__(kPickThreads, 4) void sample_pick_kernel(SampleArgs a, int segments, int bits) {
+    constexpr int BINS = kLongBins;
+    __shared__ Shared<BINS, 1> sh;
+    const int tid = threadIdx.x, n = blockIdx.x, V = a.V;
+    const Limits l(a, n);
+    const LongRow r(a.ws, n, segments);
+    const Z *row = static_cast<const Z *>(a.logits) + n * a.ld;
+    const float maximum = r.maximum<kPickThreads>(segments, sh);
+    if (l.bad() || !(maximum > -INFINITY)) { answer(a, n, -1, quiet_nan()); return; }
+    if (tid == 0) sh.word = 0x7FFFFFFF;
+    __syncthreads();
+    if (l.T == 0.f) {
+        for (int s = tid; s < segments; s += kPickThreads)
+            if (r.tops[s] == maximum) atomicMin(&sh.word, s);
+        __syncthreads();
+        const int from = sh.word * segment_words<Z>(), to = min(V, from + segment_words<Z>());
+        __syncthreads();
+        if (tid == 0) sh.word = 0x7FFFFFFF;
+        __syncthreads();
+        for (int i = from + tid; i < to; i += kPickThreads)
+            if (Row<Z>::one(row + i) == maximum) { atomicMin(&sh.word, i); break; }
+        __syncthreads();
+        answer(a, n, sh.word, 0.f);
+        return;
+    }
+    const Scale scale(l, maximum, bits, BINS);
+    Search<kPickThreads, BINS, 1> search(sh, scale, 0, V);
+    auto over_row = [&](int from, int to, auto f) {           // words in memory
+        for (int i = from + tid; i - tid < to; i += kPickThreads) f(i < to, i < to ? scale.seen(Row<Z>::one(row + i)) : -INFINITY, (uint32_t)i);
+    };
+    const bool all = lists_all(l, V), of_bin = lists_bin(l, V);
+    const int listed = all || of_bin ? *r.listed : 0;
+    auto over_list = [&](auto f) {
+        for (int i = tid; i - tid < listed; i += kPickThreads) {
+            const u64 w = i < listed ? r.list[i] : 0;
+            f(i < listed, logit_of(w), id_of(w));
+        }
+    };
+    const bool fits = listed <= kLongList;
+    u64 total;
+    if (!fits || (all || of_bin ? false : l.few(V))) {
+        total = search.all_steps(l, V, [&](auto f) { over_row(0, V, f); });
+    } else if (all) {
+        total = search.all_steps(l, V, over_list);
+    } else {
+        if (of_bin && listed) {
+            search.resolve(l.few(V) ? kCount : kWeight, *r.bin, *r.want, over_list);
+            // the words of the bin that are kept join their segments' sums
+            over_list([&](bool is, float z, uint32_t id) {
+                const u64 w = is && search.kept(z, id) ? search.weigh(kDraw, z) : 0;
+                if (w) __hip_atomic_fetch_add(&r.sums[id / segment_words<Z>()], w, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            });
+            seen_by_all();
+            __syncthreads();
+        }
+        auto sum_of = [&](int s) { return s < segments ? __hip_atomic_load(&r.sums[s], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0ull; };
+        u64 sum = 0, part;
+        for (int s = tid; s < segments; s += kPickThreads) sum += sum_of(s);
+        block_scan64<kPickThreads>(sum, sh, total);
+        const u64 target = l.target(total);
+        if (tid == 0) sh.bin = 0;
+        u64 before = 0;
+        for (int s0 = 0; s0 < segments; s0 += kPickThreads) {         // the segment that has it, and what lies in front of it
+            const u64 mine = sum_of(s0 + tid), upto = before + block_scan64<kPickThreads>(mine, sh, part);
+            if (upto - mine <= target && target < upto) { sh.bin = s0 + tid; sh.want = target - (upto - mine) + 1; }
+            before += part;
+        }
+        __syncthreads();
+        const int s = __builtin_amdgcn_readfirstlane(sh.bin), from = s * segment_words<Z>(), to = min(V, from + segment_words<Z>());
+        const u64 wanted = uniform(sh.want);
+        Search<kPickThreads, BINS, 1> inside(sh, scale, (uint32_t)from, segment_words<Z>());
+        inside.border = search.border;
+        auto over = [&](auto f) { over_row(from, to, f); };
+        inside.histogram(kDraw, over);
+        u64 want = wanted;
+        const int bin = inside.find_bin(false, want);
+        inside.resolve(kDraw, bin, want, over);
+    }
+    answer(a, n, sh.word, log_share(sh.found_w, total));
+}
+
+template <typename Z>
+int segments_of(int V) { return (V + segment_words<Z>() - 1) / segment_words<Z>(); }
+
+template <typename Z>
+hipError_t launch(const SampleArgs &a, int bits, hipStream_t stream) {
+    const int vectors = (a.V + Row<Z>::E - 1) / Row<Z>::E;
     if (vectors <= 256 * 4) sample_row_kernel<Z, 256, 4><<<a.N, 256, 0, stream>>>(a, bits);
     else if (vectors <= 1024 * 4) sample_row_kernel<Z, 1024, 4><<<a.N, 1024, 0, stream>>>(a, bits);
     else if (vectors <= 1024 * 16) sample_row_kernel<Z, 1024, 16><<<a.N, 1024, 0, stream>>>(a, bits);
-    else sample_plain_kernel<<<a.N < 65535 ? a.N : 65535, kThreads, 0, stream>>>(a, bits);
+    else {
+        const int segments = segments_of<Z>(a.V);
+        if ((long long)a.N * segments > 0x7FFFFFFF) return hipErrorInvalidValue;
+        const int groups = a.N * segments;
+        sample_tops_kernel<Z><<<groups, kSegThreads, 0, stream>>>(a, segments);
+        sample_weigh_kernel<Z><<<groups, kSegThreads, 0, stream>>>(a, segments, bits);
+        sample_gather_kernel<Z><<<groups, kSegThreads, 0, stream>>>(a, segments, bits);
+        sample_pick_kernel<Z><<<a.N, kPickThreads, 0, stream>>>(a, segments, bits);
+    }
     return hipGetLastError();
 }
+
 }  // namespace
+
+size_t sample_workspace_bytes(int N, int V) {                 // (of either type)
+    return V > 1024 * 16 * Row<float>::E ? (size_t)N * LongRow::bytes(segments_of<float>(V)) : 16;
+}
 
 hipError_t launch_sample(const SampleArgs &a, hipStream_t stream) {
     int bits = 62;                                            // sums of V weights stay below 2^62
     for (long long v = 1; v < a.V; v <<= 1) --bits;
     if (bits > 50) bits = 50;
-    return a.bf16 ? launch_rows<uint16_t>(a, bits, stream) : launch_rows<float>(a, bits, stream);
+    return a.bf16 ? launch<uint16_t>(a, bits, stream) : launch<float>(a, bits, stream);
 }
 
 }  // namespace rnnlm
