@@ -45,11 +45,13 @@ __device__ __forceinline__ double fma_with(double a, double b, double c) {
     return r;
 }
 
-// 2^y for y <= 0 as a whole number of 2^-bits, to nearest (bits <= 50; anything below -200 is nothing).  2^f on [-1/2, 1/2] is 1 + f times a
-// polynomial fitted for the least relative error, 1.5e-14; the product with 2^bits is rounded by adding 2^52, below which its last bit counts 1.
+// 2^y for y <= 0 as a whole number of 2^-bits, to nearest (bits <= 50; anything below -200 is nothing).  2^f on [-1/2, 1/2] is 1 + f times a polynomial fitted for the
+// least relative error, 1.5e-14.  Sums and products alone, at full rate: the nearest whole number n comes of adding 1.5 * 2^52 and taking it
+// off, its power of two goes into the exponent, and the result is rounded by adding 2^52, below which the last bit counts 1 (with the
+// instructions for rounding, conversion and scaling, a quarter of that rate each, 65536 weights took a workgroup 17.7 us for this).
 __device__ __forceinline__ u64 fixed_exp2(double y, int bits) {
     y = fmax(y, -200.0);
-    const double n = rint(y), f = y - n;
+    const double t = y + 0x1.8p52, f = y - (t - 0x1.8p52);
     double q = fma_with(0x1.b3de2c7e1dde3p-24, f, 0x1.63e69680bde3cp-20);
     q = fma_with(q, f, 0x1.ffce2fc63d69ep-17);
     q = fma_with(q, f, 0x1.430897f31267cp-13);
@@ -59,7 +61,9 @@ __device__ __forceinline__ u64 fixed_exp2(double y, int bits) {
     q = fma_with(q, f, 0x1.ebfbdff81be04p-3);
     q = fma_with(q, f, 0x1.62e42fefa37d1p-1);
     q = fma(q, f, 1.0);
-    return (u64)__double_as_longlong(ldexp(q, (int)n + bits) + 0x1p52) - 0x4330000000000000ull;
+    const uint32_t n = (uint32_t)__double_as_longlong(t) + (uint32_t)bits;
+    const u64 x = (u64)__double_as_longlong(q) + ((u64)(n << 20) << 32);
+    return (u64)__double_as_longlong(__longlong_as_double((long long)x) + 0x1p52) - 0x4330000000000000ull;
 }
 
 // ---- sums over a wave and a workgroup
@@ -159,6 +163,11 @@ struct Scale {
     }
     __device__ __forceinline__ float seen(float z) const { return !alike ? z : z == INFINITY ? 0.f : -INFINITY; }
     __device__ __forceinline__ u64 weight(float z) const { return fixed_exp2(((double)z - high) * per, bits); }
+    // Bounds of the logits in a bin and, for the lower one, in those in front of it, with room for the rounding of bin_of.
+    __device__ __forceinline__ float lowest(int bin) const {
+        return fmaxf(uniform(top - (float)(bin + 1) / bin_scale * (1.f + 0x1p-20f) - 0x1p-20f * fabsf(top)), -__FLT_MAX__);
+    }
+    __device__ __forceinline__ float highest(int bin) const { return uniform(top - (float)bin / bin_scale * (1.f - 0x1p-20f) + 0x1p-20f * fabsf(top)); }
     // rises as z falls; what is in the last one weighs nothing
     __device__ __forceinline__ int bin_of(float z) const {
         const float x = (top - z) * bin_scale;
@@ -214,6 +223,14 @@ template <> struct Vectors<16> {
     }
 };
 
+// M words of a thread; a logit of -infinity is no word.
+template <int N>
+struct Some {
+    static constexpr int M = N;
+    float z[N];
+    uint32_t id[N];
+};
+
 // n words from `row` on in the registers of a workgroup; elements behind them are -infinity.  A wave's vectors lie behind each other, so
 // that ids rise with wave, vector, lane, element.
 template <typename Z, int THREADS, int R>
@@ -250,61 +267,83 @@ struct Words {
 #pragma unroll
         for (int r = 0; r < R; ++r) v.set(r, loaded[r]);
     }
-    // f(index of the first element, vector as the scale sees it)
-    template <typename F> __device__ __forceinline__ void each_vector(bool alike, F f) const {
+    // f(index of the first, a vector's logits as the scale sees them), rising with vector, lane, element
+    template <typename F> __device__ __forceinline__ void vectors(bool alike, F f) const {
         v.each(used, [&](int r, u32x4 x) {
-            if (alike) {
-                float z[E];
+            float z[E];
 #pragma unroll
-                for (int j = 0; j < E; ++j) z[j] = Row<Z>::get(x, j) == INFINITY ? 0.f : -INFINITY;
-#pragma unroll
-                for (int q = 0; q < 4; ++q) x[q] = Row<Z>::pack(z, q);
+            for (int j = 0; j < E; ++j) {
+                z[j] = Row<Z>::get(x, j);
+                if (alike) z[j] = z[j] == INFINITY ? 0.f : -INFINITY;
             }
-            f((first + r * 64) * E, x);
+            f((first + r * 64) * E, z);
         });
     }
-    // f(logit, index), indices of a thread rising
-    template <typename F> __device__ __forceinline__ void each(bool alike, F f) const {
-        each_vector(alike, [&](int i, u32x4 x) {
+    // f(index of the first, four logits as the scale sees them), indices of a thread rising
+    template <typename F> __device__ __forceinline__ void fours(bool alike, F f) const {
+        v.each(used, [&](int r, u32x4 x) {
+#pragma unroll 1
+            for (int h = 0; h < E; h += 4) {
+                float z[4];
 #pragma unroll
-            for (int j = 0; j < E; ++j) f(Row<Z>::get(x, j), (uint32_t)(i + j));
+                for (int j = 0; j < 4; ++j) z[j] = E == 4 ? Row<Z>::get(x, j) : h ? Row<Z>::get(x, E - 4 + j) : Row<Z>::get(x, j);
+                if (alike)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) z[j] = z[j] == INFINITY ? 0.f : -INFINITY;
+                f((first + r * 64) * E + h, z);
+            }
+        });
+    }
+    // f(words), ids from `from` on
+    template <typename F> __device__ __forceinline__ void each(bool alike, int from, F f) const {
+        fours(alike, [&](int i, const float (&z)[4]) { f(Some<4>{{z[0], z[1], z[2], z[3]}, {(uint32_t)(from + i), (uint32_t)(from + i + 1), (uint32_t)(from + i + 2), (uint32_t)(from + i + 3)}}); });
+    }
+    // The places of all words from `low` to `high` into a list of at most `most`, `n` of them counted; a thread's behind each other.
+    __device__ __forceinline__ void list(const Scale &scale, float low, float high, int from, u64 *to, int *n, int most) const {
+        int mine = 0;
+        fours(scale.alike, [&](int, const float (&z)[4]) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) mine += z[j] >= low && z[j] <= high;
+        });
+        const int upto = wave_inclusive_scan(mine), all = __builtin_amdgcn_readlane(upto, 63);
+        if (all == 0) return;
+        int at = 0;
+        if ((threadIdx.x & 63) == 63) at = atomicAdd(n, all);
+        at = __builtin_amdgcn_readlane(at, 63) + upto - mine;
+        fours(scale.alike, [&](int i, const float (&z)[4]) {
+            bool any = false;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) any |= z[j] >= low && z[j] <= high;
+            if (!any) return;
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (z[j] >= low && z[j] <= high) {
+                    if (at < most) to[at] = place(z[j], (uint32_t)(from + i + j));
+                    ++at;
+                }
         });
     }
     // This thread's largest logit; NaN where there is one.
     __device__ __forceinline__ float largest() const {
         float high = -INFINITY;
         bool nan = false;
-        each(false, [&](float z, uint32_t) { high = fmaxf(high, z); nan |= z != z; });
+        v.each(used, [&](int, u32x4 x) {
+#pragma unroll
+            for (int j = 0; j < E; ++j) {
+                const float z = Row<Z>::get(x, j);
+                high = fmaxf(high, z);
+                nan |= z != z;
+            }
+        });
         return nan ? quiet_nan() : high;
     }
 };
-
-// Appends words to a list of at most `most`; beyond that they are only counted in `n`.  put(i, to): which of this thread's M words goes where.
-template <int M>
-struct Taken { bool is[M]; };
-template <int M, typename F>
-__device__ __forceinline__ void append(int *n, const Taken<M> &take, int most, F put) {
-    const int lane = threadIdx.x & 63;
-    u64 who[M];
-    int all = 0, at = 0;
-#pragma unroll
-    for (int i = 0; i < M; ++i) { who[i] = __ballot(take.is[i]); all += __popcll(who[i]); }
-    if (all == 0) return;
-    if (lane == 0) at = atomicAdd(n, all);
-    at = __builtin_amdgcn_readfirstlane(at);
-#pragma unroll
-    for (int i = 0; i < M; ++i) {
-        const int to = at + __popcll(who[i] & ((1ull << lane) - 1));
-        if (take.is[i] && to < most) put(i, to);
-        at += __popcll(who[i]);
-    }
-}
 
 // ---- the search for a prefix
 
 enum Kind { kCount, kWeight, kDraw };        // top_k: words, by place.  top_p: weight, by place.  The draw: weight of at least `least`, by id.
 
-// `over(f)` calls f(there, logit, id) for the words of a source (registers, a list, memory), the same number of times in all lanes of a wave.
+// `over(f)` calls f(words) for the words of a source (registers, a list, memory), the same number of times in all lanes of a wave.
 template <int THREADS, int BINS, int LIST>
 struct Search {
     static constexpr int kPerThread = BINS / THREADS, WAVES = THREADS / 64;
@@ -323,39 +362,43 @@ struct Search {
     }
     __device__ __forceinline__ int bin_at(Kind kind, float z, uint32_t id) const { return kind == kDraw ? (int)((id - id_from) >> id_shift) : scale.bin_of(z); }
     __device__ __forceinline__ u64 order(Kind kind, float z, uint32_t id) const { return kind == kDraw ? ~(u64)id : place(z, id); }
-    __device__ __forceinline__ void clear() {
-        __syncthreads();
+    // Histogram of the words kept.  (Whoever read the last one did so in front of a barrier.)
+    template <typename O>
+    __device__ __forceinline__ void histogram(Kind kind, O over) {
         for (int i = threadIdx.x; i < BINS; i += THREADS) sh.weight[i] = 0;
         __syncthreads();
-    }
-    // Histogram of the words kept; returns their weight (nothing of use for counts).
-    template <typename O>
-    __device__ __forceinline__ u64 histogram(Kind kind, O over) {
-        clear();
-        u64 sum = 0, total;
-        if (kind != kCount) over([&](bool is, float z, uint32_t id) {
-            u64 w = scale.weight(z);
-            w = is && kept(z, id) && !(kind == kDraw && w < scale.least) ? w : 0;
-            sum += w;
-            if (w) atomicAdd(&sh.weight[bin_at(kind, z, id)], w);
+        if (kind != kCount) over([&](auto some) {
+#pragma unroll
+            for (int j = 0; j < some.M; ++j) {
+                u64 w = scale.weight(some.z[j]);
+                w = kept(some.z[j], some.id[j]) && !(kind == kDraw && w < scale.least) ? w : 0;
+                if (w) atomicAdd(&sh.weight[bin_at(kind, some.z[j], some.id[j])], w);
+            }
         });
-        else over([&](bool is, float z, uint32_t id) {
-            if (is && kept(z, id)) atomicAdd(&sh.count[scale.bin_of(z)], 1);
+        else over([&](auto some) {
+#pragma unroll
+            for (int j = 0; j < some.M; ++j)
+                if (kept(some.z[j], some.id[j])) atomicAdd(&sh.count[scale.bin_of(some.z[j])], 1);
         });
-        block_scan64<THREADS>(sum, sh, total);
-        return total;
+        __syncthreads();
     }
-    // The bin where `want` of the histogram is reached from the front (the last one if it is not), and what is still wanted of that bin.
-    __device__ __forceinline__ int find_bin(bool counts, u64 &want) {
+    // The bin where want_of(all of the histogram) is reached from the front (the last one if it is not), and what is still wanted of that bin.
+    template <typename F>
+    __device__ __forceinline__ int find_bin(bool counts, u64 &want, u64 &total, F want_of) {
         const int tid = threadIdx.x;
-        u64 h[kPerThread], sum = 0, total;
+        u64 h[kPerThread], sum = 0;
 #pragma unroll
         for (int i = 0; i < kPerThread; ++i) {
             h[i] = counts ? (u64)sh.count[tid * kPerThread + i] : sh.weight[tid * kPerThread + i];
             sum += h[i];
         }
-        if (tid == 0) { sh.bin = BINS - 1; sh.want = want; }
         u64 upto = block_scan64<THREADS>(sum, sh, total) - sum;
+        want = want_of(total);
+        if (tid == 0) {
+            sh.n = 0;                                         // of the bin's words, for resolve()
+            sh.border = border;
+            if (total < want) { sh.bin = BINS - 1; sh.want = want; }
+        }
         if (upto < want && upto + sum >= want) {
 #pragma unroll
             for (int i = 0; i < kPerThread; ++i) {
@@ -367,34 +410,46 @@ struct Search {
         want = uniform(sh.want);
         return __builtin_amdgcn_readfirstlane(sh.bin);
     }
-    // Of the words of `bin` the one at which `want` is reached: the new border, or the word drawn (sh.word, sh.found_w).
+    // Of the words of `bin` the one at which `want` is reached: the new border, or the word drawn (sh.word, sh.found_w).  Behind find_bin().
     template <typename O>
     __device__ __forceinline__ void resolve(Kind kind, int bin, u64 want, O over) {
         const int tid = threadIdx.x, lane = tid & 63;
         u64 low = 0, high = ~0ull;                            // of the orders
-        auto inside = [&](bool is, float z, uint32_t id) {
-            const bool yes = is && bin_at(kind, z, id) == bin;
-            if (!__any(yes)) return false;                    // (most vectors have no word of one bin)
+        const float low_z = kind == kDraw ? -INFINITY : scale.lowest(bin), high_z = kind == kDraw ? INFINITY : scale.highest(bin);
+        auto inside = [&](float z, uint32_t id) {
             const u64 o = order(kind, z, id);
-            return yes && kept(z, id) && o >= low && o <= high;
+            return bin_at(kind, z, id) == bin && kept(z, id) && o >= low && o <= high;
+        };
+        // f(which are inside, words), where there are any
+        auto insiders = [&](auto f) {
+            over([&](auto some) {
+                constexpr int M = decltype(some)::M;
+                bool any = false;                             // (most batches have no word of one bin)
+#pragma unroll
+                for (int j = 0; j < M; ++j) any |= kind == kDraw ? bin_at(kind, some.z[j], some.id[j]) == bin : some.z[j] >= low_z && some.z[j] <= high_z;
+                if (!__any(any)) return;
+#pragma unroll
+                for (int j = 0; j < M; ++j) f(inside(some.z[j], some.id[j]), some.z[j], some.id[j]);
+            });
         };
         while (true) {
-            __syncthreads();
-            if (tid == 0) sh.n = 0;
-            __syncthreads();
             u64 least_o = ~0ull, most_o = 0;
-            over([&](bool is, float z, uint32_t id) {
-                const Taken<1> take = {{inside(is, z, id)}};
-                if (!__any(take.is[0])) return;
+            insiders([&](bool is, float z, uint32_t id) {
+                const u64 who = __ballot(is);
+                if (who == 0) return;
+                int at = 0;
+                if (lane == 0) at = atomicAdd(&sh.n, __popcll(who));
                 const u64 o = order(kind, z, id);
-                if (take.is[0]) { least_o = o < least_o ? o : least_o; most_o = o > most_o ? o : most_o; }
-                append(&sh.n, take, kSmall, [&](int, int to) { sh.small[to] = o; sh.small_w[to] = weigh(kind, z); });
+                at = __builtin_amdgcn_readfirstlane(at) + __popcll(who & ((1ull << lane) - 1));
+                if (is) {
+                    least_o = o < least_o ? o : least_o;
+                    most_o = o > most_o ? o : most_o;
+                    if (at < kSmall) { sh.small[at] = o; sh.small_w[at] = weigh(kind, z); }
+                }
             });
             __syncthreads();
             const int some = __builtin_amdgcn_readfirstlane(sh.n);
             if (some <= kSmall) {
-                if (tid == 0) sh.border = border;
-                __syncthreads();
                 if (tid < some) {
                     const u64 o = sh.small[tid], w = sh.small_w[tid];
                     u64 before = 0;
@@ -412,7 +467,8 @@ struct Search {
                 most_o = h > most_o ? h : most_o;
             }
             if (lane == 0) { sh.low64[tid >> 6] = least_o; sh.high64[tid >> 6] = most_o; }
-            clear();
+            for (int i = tid; i < BINS; i += THREADS) sh.weight[i] = 0;
+            __syncthreads();
             low = ~0ull;
             high = 0;
             for (int w = 0; w < WAVES; ++w) {
@@ -423,14 +479,16 @@ struct Search {
             high = uniform(high);
             int shift = 0;
             while ((high - low) >> shift >= (u64)BINS) ++shift;
-            over([&](bool is, float z, uint32_t id) {
-                if (!inside(is, z, id)) return;
+            insiders([&](bool is, float z, uint32_t id) {
+                if (!is) return;
                 const int at = (int)((high - order(kind, z, id)) >> shift);
                 if (kind == kCount) atomicAdd(&sh.count[at], 1);
                 else atomicAdd(&sh.weight[at], weigh(kind, z));
             });
             __syncthreads();
-            high -= (u64)find_bin(kind == kCount, want) << shift;
+            u64 total;
+            const u64 still = want;
+            high -= (u64)find_bin(kind == kCount, want, total, [&](u64) { return still; }) << shift;
             const u64 more = (1ull << shift) - 1;
             if (high - low > more) low = high - more;
         }
@@ -438,9 +496,9 @@ struct Search {
     // One limit, or the draw: the weight of all words it was made of (0 where nothing had to be searched).
     template <typename O>
     __device__ __forceinline__ u64 step(Kind kind, const Limits &l, O over) {
-        const u64 total = histogram(kind, over);
-        u64 want = kind == kCount ? (u64)l.k : kind == kWeight ? l.want_p(total) : l.target(total) + 1;
-        const int bin = find_bin(kind == kCount, want);
+        histogram(kind, over);
+        u64 want, total;
+        const int bin = find_bin(kind == kCount, want, total, [&](u64 all) { return kind == kCount ? (u64)l.k : kind == kWeight ? l.want_p(all) : l.target(all) + 1; });
         if (bin < BINS - 1 || kind == kDraw) resolve(kind, bin, want, over);      // in the last bin nothing has a weight
         return total;
     }
@@ -463,54 +521,60 @@ __device__ __forceinline__ void answer(const SampleArgs &a, int n, int word, flo
 }
 __device__ __forceinline__ float log_share(u64 w, u64 total) { return (float)log((double)w / (double)total); }
 
-// The draw among n words in registers that `border` keeps, in the order of the ids: sums of threads, of the vectors of the wave that has it, of
-// its lanes, of the lane's words.
-template <int THREADS, typename W, typename S>
-__device__ __forceinline__ u64 draw_from_registers(const W &words, S &sh, const Scale &scale, const Limits &l, u64 border) {
-    constexpr int E = W::E;
+// The draw among words in registers, ids from `from` on, that `border` keeps, in the order of the ids: sums of threads, of the vectors of the wave
+// that has it, of its lanes, of the lane's words.  target_of(their weight) is what the sum has to pass.
+template <int THREADS, typename W, typename S, typename F>
+__device__ __forceinline__ u64 draw_from_registers(const W &words, S &sh, const Scale &scale, const Limits &l, u64 border, int from, F target_of) {
     // no word below it is kept (by min_p: of a weight of `least` at least, with a hundredth of a factor of two for what logarithm and bound are off)
     float floor_z = border ? logit_of(border) : -INFINITY;
     if (scale.least) floor_z = fmaxf(floor_z, (float)(scale.high + ((double)log2f(fminf(l.mp, 1.f)) - 0.01) / scale.per) - 1e-6f * fabsf(scale.top));
     floor_z = uniform(floor_z);
-    u64 w[E];
-    auto weigh = [&](int i, u32x4 x) {
+    auto weigh = [&](int i, const float (&z)[4], u64 (&w)[4]) {
         u64 s = 0;
-        float high = Row<typename W::Type>::get(x, 0);
+        const float high = fmaxf(fmaxf(z[0], z[1]), fmaxf(z[2], z[3]));
 #pragma unroll
-        for (int j = 1; j < E; ++j) high = fmaxf(high, Row<typename W::Type>::get(x, j));
-#pragma unroll
-        for (int j = 0; j < E; ++j) w[j] = 0;
+        for (int j = 0; j < 4; ++j) w[j] = 0;
         if (!__any(high >= floor_z && high > -INFINITY)) return s;
 #pragma unroll
-        for (int j = 0; j < E; ++j) w[j] = scale.weight(Row<typename W::Type>::get(x, j));
+        for (int j = 0; j < 4; ++j) w[j] = scale.weight(z[j]);
         if (border)
 #pragma unroll
-            for (int j = 0; j < E; ++j)
-                if (place(Row<typename W::Type>::get(x, j), (uint32_t)(i + j)) < border) w[j] = 0;
+            for (int j = 0; j < 4; ++j)
+                if (place(z[j], (uint32_t)(from + i + j)) < border) w[j] = 0;
         if (scale.least)
 #pragma unroll
-            for (int j = 0; j < E; ++j)
+            for (int j = 0; j < 4; ++j)
                 if (w[j] < scale.least) w[j] = 0;
 #pragma unroll
-        for (int j = 0; j < E; ++j) s += w[j];
+        for (int j = 0; j < 4; ++j) s += w[j];
         return s;
     };
     u64 sum = 0, total;
-    words.each_vector(scale.alike, [&](int i, u32x4 x) { sum += weigh(i, x); });
-    const u64 upto_wave = of_lane(block_scan64<THREADS>(sum, sh, total), 63), target = l.target(total);
+    words.fours(scale.alike, [&](int i, const float (&z)[4]) {
+        u64 w[4];
+        sum += weigh(i, z, w);
+    });
+    const u64 upto_wave = of_lane(block_scan64<THREADS>(sum, sh, total), 63), target = target_of(total);
     u64 before = upto_wave - of_lane(wave_scan64(sum), 63);
     if (before <= target && target < upto_wave) {
         bool done = false;
-        words.each_vector(scale.alike, [&](int i, u32x4 x) {
+        words.vectors(scale.alike, [&](int i, const float (&z)[W::E]) {
             if (done) return;
-            const u64 s = weigh(i, x), upto = before + wave_scan64(s), all = of_lane(upto, 63);
+            u64 w[W::E / 4][4], s = 0;
+#pragma unroll
+            for (int h = 0; h < W::E / 4; ++h) {
+                const float four[4] = {z[4 * h], z[4 * h + 1], z[4 * h + 2], z[4 * h + 3]};
+                s += weigh(i + 4 * h, four, w[h]);
+            }
+            const u64 upto = before + wave_scan64(s), all = of_lane(upto, 63);
             if (all > target) {
                 u64 at = upto - s;
                 if (at <= target && target < upto) {
 #pragma unroll
-                    for (int j = 0; j < E; ++j) {
-                        if (at <= target && target < at + w[j]) { sh.word = i + j; sh.found_w = w[j]; }
-                        at += w[j];
+                    for (int j = 0; j < W::E; ++j) {
+                        const u64 x = w[j / 4][j % 4];
+                        if (at <= target && target < at + x) { sh.word = from + i + j; sh.found_w = x; }
+                        at += x;
                     }
                 }
                 done = true;
@@ -525,7 +589,7 @@ __device__ __forceinline__ u64 draw_from_registers(const W &words, S &sh, const 
 // A row in the registers of one workgroup.
 template <typename Z, int THREADS, int R>
 __global__ __launch_bounds__(THREADS, 4) void sample_row_kernel(SampleArgs a, int bits) {
-    constexpr int BINS = bins_of(THREADS), LIST = list_of(THREADS), E = Row<Z>::E;
+    constexpr int BINS = bins_of(THREADS), LIST = list_of(THREADS);
     __shared__ Shared<BINS, LIST> sh;
     const int tid = threadIdx.x, n = blockIdx.x, V = a.V;
     const Limits l(a, n);
@@ -538,7 +602,10 @@ __global__ __launch_bounds__(THREADS, 4) void sample_row_kernel(SampleArgs a, in
     if (nan || l.bad() || maximum == -INFINITY) { answer(a, n, -1, quiet_nan()); return; }
     if (l.T == 0.f) {
         uint32_t at = 0x7FFFFFFF;
-        if (__any(mine == maximum)) words.each(false, [&](float z, uint32_t id) { at = z == maximum && id < at ? id : at; });
+        if (__any(mine == maximum)) words.each(false, 0, [&](auto some) {
+#pragma unroll
+            for (int j = 0; j < some.M; ++j) at = some.z[j] == maximum && some.id[j] < at ? some.id[j] : at;
+        });
         if (at != 0x7FFFFFFF) atomicMin(&sh.word, (int)at);
         __syncthreads();
         answer(a, n, sh.word, 0.f);
@@ -554,15 +621,10 @@ __global__ __launch_bounds__(THREADS, 4) void sample_row_kernel(SampleArgs a, in
     if (l.few(V) && l.k <= THREADS / 2) {
         if (mine > -INFINITY) atomicAdd(&sh.count[scale.bin_of(mine)], 1);
         __syncthreads();
-        u64 want = (u64)l.k;
-        const int edge = search.find_bin(true, want);
+        u64 want, all;
+        const int edge = search.find_bin(true, want, all, [&](u64) { return (u64)l.k; });
         if (edge < BINS - 1) {
-            words.each_vector(scale.alike, [&](int i, u32x4 x) {
-                Taken<E> take;
-#pragma unroll
-                for (int j = 0; j < E; ++j) take.is[j] = (scale.top - Row<Z>::get(x, j)) * scale.bin_scale < (float)(edge + 1);
-                append(&sh.n, take, LIST, [&](int j, int to) { sh.list[to] = place(Row<Z>::get(x, j), (uint32_t)(i + j)); });
-            });
+            words.list(scale, scale.lowest(edge), INFINITY, 0, sh.list, &sh.n, LIST);
             __syncthreads();
             listed = __builtin_amdgcn_readfirstlane(sh.n);
             in_list = listed <= LIST;
@@ -572,22 +634,25 @@ __global__ __launch_bounds__(THREADS, 4) void sample_row_kernel(SampleArgs a, in
         if (in_list)
             for (int i = tid; i - tid < listed; i += THREADS) {
                 const u64 w = i < listed ? sh.list[i] : 0;
-                f(i < listed, logit_of(w), id_of(w));
+                f(Some<1>{{i < listed ? logit_of(w) : -INFINITY}, {id_of(w)}});
             }
-        else words.each(scale.alike, [&](float z, uint32_t id) { f(id < (uint32_t)V, z, id); });
+        else words.each(scale.alike, 0, f);
     };
     u64 total = 0;
 #pragma unroll 1
     for (int kind = kCount; kind <= kDraw; ++kind)
         if (kind == kCount ? l.few(V) : kind == kWeight ? l.part() : in_list) total = search.step((Kind)kind, l, over);
-    if (!in_list) total = draw_from_registers<THREADS>(words, sh, scale, l, search.border);
+    if (!in_list) total = draw_from_registers<THREADS>(words, sh, scale, l, search.border, 0, [&](u64 all) { return l.target(all); });
     answer(a, n, sh.word, log_share(sh.found_w, total));
 }
 
 // ---- rows in segments
 
-constexpr int kSegThreads = 256, kSegVectors = 16, kLongBins = 4096, kLongList = 8192, kPickThreads = 1024;
+constexpr int kSegThreads = 256, kSegVectors = 16, kLongBins = 4096, kPickThreads = 1024;
 template <typename Z> constexpr int segment_words() { return kSegThreads * kSegVectors * Row<Z>::E; }
+
+// Words that can be listed of a row in memory.  In bfloat16 a bin is one logit, and some hundredth of the words may have it.
+__host__ __device__ constexpr int long_list(int V) { return V / 16 > 8192 ? V / 16 : 8192; }
 
 // Of one row in the workspace, behind its histogram of kLongBins weights (or counts): the deciding bin and what is wanted of it, the words listed,
 // how many there are, and of every segment its maximum and the weight of its words that are kept for certain.
@@ -596,12 +661,12 @@ struct LongRow {
     u64 *want;
     int *bin, *listed;
     float *tops;
-    static __host__ __device__ size_t bytes(int segments) { return (size_t)(kLongBins + kLongList + segments) * 8 + 16 + ((size_t)segments * 4 + 15) / 16 * 16; }
-    __device__ LongRow(void *ws, int n, int segments) {
-        char *p = static_cast<char *>(ws) + n * bytes(segments);
+    static __host__ __device__ size_t bytes(int V, int segments) { return (size_t)(kLongBins + long_list(V) + segments) * 8 + 16 + ((size_t)segments * 4 + 15) / 16 * 16; }
+    __device__ LongRow(void *ws, int n, int V, int segments) {
+        char *p = static_cast<char *>(ws) + n * bytes(V, segments);
         hist = reinterpret_cast<u64 *>(p);
         list = hist + kLongBins;
-        sums = list + kLongList;
+        sums = list + long_list(V);
         want = sums + segments;
         bin = reinterpret_cast<int *>(want + 1);
         listed = bin + 1;
@@ -624,14 +689,14 @@ struct LongRow {
 };
 // Of a row with top_k all words that can be kept are listed, and the last launch does the rest, unless they are too many; then, and with top_p alone,
 // the words of the deciding bin.  (Too many with top_p as well: the last launch reads the row itself.)
-__device__ __forceinline__ bool lists_all(const Limits &l, int V) { return l.few(V) && l.k <= kLongList / 2; }
+__device__ __forceinline__ bool lists_all(const Limits &l, int V) { return l.few(V) && l.k <= long_list(V) / 2; }
 __device__ __forceinline__ bool lists_bin(const Limits &l, int V) { return l.few(V) ? !lists_all(l, V) && !l.part() : l.part(); }
 
 template <typename Z>
 __global__ __launch_bounds__(kSegThreads) void sample_tops_kernel(SampleArgs a, int segments) {
     __shared__ Shared<16, 1> sh;
     const int n = blockIdx.x / segments, s = blockIdx.x % segments, from = s * segment_words<Z>(), len = min(a.V - from, segment_words<Z>());
-    const LongRow r(a.ws, n, segments);
+    const LongRow r(a.ws, n, a.V, segments);
     const Words<Z, kSegThreads, kSegVectors> words(static_cast<const Z *>(a.logits) + n * a.ld + from, len);
     for (int i = s * kSegThreads + threadIdx.x; i < kLongBins; i += segments * kSegThreads) r.hist[i] = 0;
     if (s == 0 && threadIdx.x == 0) *r.listed = 0;
@@ -646,16 +711,22 @@ __global__ __launch_bounds__(kSegThreads) void sample_weigh_kernel(SampleArgs a,
     __shared__ Shared<kLongBins, 1> sh;
     const int n = blockIdx.x / segments, s = blockIdx.x % segments, from = s * segment_words<Z>(), len = min(a.V - from, segment_words<Z>());
     const Limits l(a, n);
-    const LongRow r(a.ws, n, segments);
+    const LongRow r(a.ws, n, a.V, segments);
     const Words<Z, kSegThreads, kSegVectors> words(static_cast<const Z *>(a.logits) + n * a.ld + from, len);
     const float maximum = r.maximum<kSegThreads>(segments, sh);
     if (l.bad() || !(maximum > -INFINITY) || l.T == 0.f) return;
     const Scale scale(l, maximum, bits, kLongBins);
     Search<kSegThreads, kLongBins, 1> search(sh, scale, 0, a.V);
-    auto over = [&](auto f) { words.each(scale.alike, [&](float z, uint32_t id) { f(id < (uint32_t)len, z, id); }); };
+    auto over = [&](auto f) { words.each(scale.alike, from, f); };
     if (!l.few(a.V) && !l.part()) {
         u64 sum = 0, total;
-        over([&](bool is, float z, uint32_t) { sum += is ? search.weigh(kDraw, z) : 0; });
+        over([&](auto some) {
+#pragma unroll
+            for (int j = 0; j < some.M; ++j) {
+                const u64 w = search.weigh(kDraw, some.z[j]);
+                sum += some.z[j] > -INFINITY ? w : 0;
+            }
+        });
         block_scan64<kSegThreads>(sum, sh, total);
         if (threadIdx.x == 0) r.sums[s] = total;
         return;
@@ -670,52 +741,39 @@ __global__ __launch_bounds__(kSegThreads) void sample_weigh_kernel(SampleArgs a,
 
 template <typename Z>
 __global__ __launch_bounds__(kSegThreads) void sample_gather_kernel(SampleArgs a, int segments, int bits) {
-    constexpr int E = Row<Z>::E;
     __shared__ Shared<kLongBins, 1> sh;
     const int tid = threadIdx.x, n = blockIdx.x / segments, s = blockIdx.x % segments, from = s * segment_words<Z>(), len = min(a.V - from, segment_words<Z>());
     const Limits l(a, n);
     const bool all = lists_all(l, a.V);
     if (!all && !lists_bin(l, a.V)) return;
-    const LongRow r(a.ws, n, segments);
+    const LongRow r(a.ws, n, a.V, segments);
     const Words<Z, kSegThreads, kSegVectors> words(static_cast<const Z *>(a.logits) + n * a.ld + from, len);
     const float maximum = r.maximum<kSegThreads>(segments, sh);
     if (l.bad() || !(maximum > -INFINITY) || l.T == 0.f) return;
     const Scale scale(l, maximum, bits, kLongBins);
     Search<kSegThreads, kLongBins, 1> search(sh, scale, 0, a.V);
-    u64 sum = 0, total;
+    u64 h[kLongBins / kSegThreads], want, total;               // (all on their way at once)
+#pragma unroll
+    for (int i = 0; i < kLongBins / kSegThreads; ++i) h[i] = r.hist[i * kSegThreads + tid];
+#pragma unroll
+    for (int i = 0; i < kLongBins / kSegThreads; ++i) sh.weight[i * kSegThreads + tid] = h[i];
     __syncthreads();
-    for (int i = tid; i < kLongBins; i += kSegThreads) {
-        sh.weight[i] = r.hist[i];
-        sum += sh.weight[i];
-    }
-    block_scan64<kSegThreads>(sum, sh, total);
-    u64 want = l.few(a.V) ? (u64)l.k : l.want_p(total);
-    const int bin = search.find_bin(false, want);
+    const int bin = search.find_bin(false, want, total, [&](u64 all_of_it) { return l.few(a.V) ? (u64)l.k : l.want_p(all_of_it); });
     if (s == 0 && tid == 0) { *r.bin = bin; *r.want = want; }
-    // The words of the bin, or all up to it; a whole wave's words take one number from the row's counter.
-    words.each_vector(scale.alike, [&](int i, u32x4 x) {
-        Taken<E> take;
-        bool any = false;
-#pragma unroll
-        for (int j = 0; j < E; ++j) {
-            const float z = Row<Z>::get(x, j);
-            const int b = scale.bin_of(z);
-            take.is[j] = z > -INFINITY && i + j < len && (all ? b <= bin : b == bin && bin < kLongBins - 1);
-            any |= take.is[j];
-        }
-        if (__any(any)) append(r.listed, take, kLongList, [&](int j, int to) { r.list[to] = place(Row<Z>::get(x, j), (uint32_t)(from + i + j)); });
-    });
+    // The words of the bin (a few more do no harm), or all up to it, and the weight of those in front of it.
+    const float low = scale.lowest(bin);
+    if (all || bin < kLongBins - 1) words.list(scale, low, all ? INFINITY : scale.highest(bin), from, r.list, r.listed, long_list(a.V));
     if (all) return;
-    sum = 0;
-    words.each_vector(scale.alike, [&](int i, u32x4 x) {
+    u64 sum = 0;
+    words.each(scale.alike, from, [&](auto some) {
         bool any = false;
 #pragma unroll
-        for (int j = 0; j < E; ++j) any |= scale.bin_of(Row<Z>::get(x, j)) < bin;
+        for (int j = 0; j < some.M; ++j) any |= some.z[j] >= low;
         if (!__any(any)) return;
 #pragma unroll
-        for (int j = 0; j < E; ++j) {
-            const float z = Row<Z>::get(x, j);
-            sum += scale.bin_of(z) < bin ? search.weigh(kDraw, z) : 0;
+        for (int j = 0; j < some.M; ++j) {
+            const u64 w = search.weigh(kDraw, some.z[j]);
+            sum += some.z[j] > -INFINITY && scale.bin_of(some.z[j]) < bin ? w : 0;
         }
     });
     block_scan64<kSegThreads>(sum, sh, total);
@@ -728,7 +786,7 @@ __global__ __launch_bounds__(kPickThreads, 4) void sample_pick_kernel(SampleArgs
     __shared__ Shared<BINS, 1> sh;
     const int tid = threadIdx.x, n = blockIdx.x, V = a.V;
     const Limits l(a, n);
-    const LongRow r(a.ws, n, segments);
+    const LongRow r(a.ws, n, a.V, segments);
     const Z *row = static_cast<const Z *>(a.logits) + n * a.ld;
     const float maximum = r.maximum<kPickThreads>(segments, sh);
     if (l.bad() || !(maximum > -INFINITY)) { answer(a, n, -1, quiet_nan()); return; }
@@ -750,35 +808,71 @@ __global__ __launch_bounds__(kPickThreads, 4) void sample_pick_kernel(SampleArgs
     }
     const Scale scale(l, maximum, bits, BINS);
     Search<kPickThreads, BINS, 1> search(sh, scale, 0, V);
-    auto over_row = [&](int from, int to, auto f) {           // words in memory
-        for (int i = from + tid; i - tid < to; i += kPickThreads) f(i < to, i < to ? scale.seen(Row<Z>::one(row + i)) : -INFINITY, (uint32_t)i);
+    // Words in memory, eight of a thread on their way at once.
+    auto over_row = [&](auto f) {
+        for (int i0 = 0; i0 < V; i0 += 8 * kPickThreads) {
+            float z[8];
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+                const int i = i0 + q * kPickThreads + tid;
+                z[q] = i < V ? scale.seen(Row<Z>::one(row + i)) : -INFINITY;
+            }
+#pragma unroll 1
+            for (int q = 0; q < 8; ++q) {
+                float x = z[0];
+#pragma unroll
+                for (int p = 1; p < 8; ++p) x = q == p ? z[p] : x;
+                const int i = i0 + q * kPickThreads + tid;
+                f(Some<1>{{x}, {(uint32_t)i}});
+            }
+        }
     };
     const bool all = lists_all(l, V), of_bin = lists_bin(l, V);
     const int listed = all || of_bin ? *r.listed : 0;
     auto over_list = [&](auto f) {
-        for (int i = tid; i - tid < listed; i += kPickThreads) {
-            const u64 w = i < listed ? r.list[i] : 0;
-            f(i < listed, logit_of(w), id_of(w));
+        for (int i0 = 0; i0 < listed; i0 += 8 * kPickThreads) {
+            u64 w[8];
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+                const int i = i0 + q * kPickThreads + tid;
+                w[q] = i < listed ? r.list[i] : 0;
+            }
+#pragma unroll 1
+            for (int q = 0; q < 8 && i0 + q * kPickThreads < listed; ++q) {
+                u64 x = w[0];
+#pragma unroll
+                for (int p = 1; p < 8; ++p) x = q == p ? w[p] : x;
+                f(Some<1>{{i0 + q * kPickThreads + tid < listed ? logit_of(x) : -INFINITY}, {id_of(x)}});
+            }
         }
     };
-    const bool fits = listed <= kLongList;
+    const bool fits = listed <= long_list(V);
     u64 total;
     if (!fits || (all || of_bin ? false : l.few(V))) {
-        total = search.all_steps(l, V, [&](auto f) { over_row(0, V, f); });
+        total = search.all_steps(l, V, over_row);
     } else if (all) {
         total = search.all_steps(l, V, over_list);
     } else {
+        const bool in_lds = segments <= BINS;                 // what the bin's words add to the segments' sums
+        for (int i = tid; i < BINS; i += kPickThreads) sh.weight[i] = 0;
         if (of_bin && listed) {
-            search.resolve(l.few(V) ? kCount : kWeight, *r.bin, *r.want, over_list);
-            // the words of the bin that are kept join their segments' sums
-            over_list([&](bool is, float z, uint32_t id) {
-                const u64 w = is && search.kept(z, id) ? search.weigh(kDraw, z) : 0;
-                if (w) __hip_atomic_fetch_add(&r.sums[id / segment_words<Z>()], w, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            const int bin = *r.bin;
+            if (tid == 0) { sh.n = 0; sh.border = 0; }
+            __syncthreads();
+            search.resolve(l.few(V) ? kCount : kWeight, bin, *r.want, over_list);
+            for (int i = tid; i < BINS; i += kPickThreads) sh.weight[i] = 0;
+            __syncthreads();
+            over_list([&](auto some) {
+                if (!search.kept(some.z[0], some.id[0]) || scale.bin_of(some.z[0]) != bin) return;
+                const u64 w = search.weigh(kDraw, some.z[0]);
+                const int s = some.id[0] / segment_words<Z>();
+                if (in_lds) atomicAdd(&sh.weight[s], w);
+                else __hip_atomic_fetch_add(&r.sums[s], w, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
             });
             seen_by_all();
-            __syncthreads();
         }
-        auto sum_of = [&](int s) { return s < segments ? __hip_atomic_load(&r.sums[s], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0ull; };
+        __syncthreads();
+        auto sum_of = [&](int s) { return s < segments ? __hip_atomic_load(&r.sums[s], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + (in_lds ? sh.weight[s] : 0) : 0ull; };
         u64 sum = 0, part;
         for (int s = tid; s < segments; s += kPickThreads) sum += sum_of(s);
         block_scan64<kPickThreads>(sum, sh, total);
@@ -793,13 +887,8 @@ __global__ __launch_bounds__(kPickThreads, 4) void sample_pick_kernel(SampleArgs
         __syncthreads();
         const int s = __builtin_amdgcn_readfirstlane(sh.bin), from = s * segment_words<Z>(), to = min(V, from + segment_words<Z>());
         const u64 wanted = uniform(sh.want);
-        Search<kPickThreads, BINS, 1> inside(sh, scale, (uint32_t)from, segment_words<Z>());
-        inside.border = search.border;
-        auto over = [&](auto f) { over_row(from, to, f); };
-        inside.histogram(kDraw, over);
-        u64 want = wanted;
-        const int bin = inside.find_bin(false, want);
-        inside.resolve(kDraw, bin, want, over);
+        const Words<Z, kPickThreads, kSegThreads * kSegVectors / kPickThreads> words(row + from, to - from);
+        draw_from_registers<kPickThreads>(words, sh, scale, l, search.border, from, [&](u64) { return wanted - 1; });
     }
     answer(a, n, sh.word, log_share(sh.found_w, total));
 }
@@ -828,7 +917,7 @@ hipError_t launch(const SampleArgs &a, int bits, hipStream_t stream) {
 }  // namespace
 
 size_t sample_workspace_bytes(int N, int V) {                 // (of either type)
-    return V > 1024 * 16 * Row<float>::E ? (size_t)N * LongRow::bytes(segments_of<float>(V)) : 16;
+    return V > 1024 * 16 * Row<float>::E ? (size_t)N * LongRow::bytes(V, segments_of<float>(V)) : 16;
 }
 
 hipError_t launch_sample(const SampleArgs &a, hipStream_t stream) {
