@@ -90,8 +90,11 @@ __device__ __forceinline__ u64 of_lane(u64 v, int lane) {
 // Bins of the distance to the row's maximum, over the kOctaves factors of two in which a weight is not nothing; words that can be listed;
 // words that are put in order by comparing each with each.
 constexpr int kOctaves = 52, kSmall = 256;
-constexpr int bins_of(int threads) { return threads > 256 ? 4096 : 1024; }
-constexpr int list_of(int threads) { return threads > 256 ? 2048 : 512; }
+// (16384 bins leave the deciding one of 65536 words some 30 of them; of 4096 it had over kSmall in flat rows, and took three passes more.)
+constexpr int bins_of(int words) { return words > 16384 ? 16384 : words > 4096 ? 4096 : 1024; }
+constexpr int list_of(int words) { return words > 4096 ? 2048 : 512; }
+// Where bin b is: a thread's bins lie behind each other, and the threads of a wave read theirs from different banks.
+__device__ __forceinline__ int slot(int b) { return b ^ (b >> 4 & 15); }
 
 template <int BINS, int LIST>
 struct Shared {
@@ -302,6 +305,7 @@ struct Words {
     __device__ __forceinline__ void list(const Scale &scale, float low, float high, int from, u64 *to, int *n, int most) const {
         int mine = 0;
         fours(scale.alike, [&](int, const float (&z)[4]) {
+            if (!__any(fmaxf(fmaxf(z[0], z[1]), fmaxf(z[2], z[3])) >= low)) return;
 #pragma unroll
             for (int j = 0; j < 4; ++j) mine += z[j] >= low && z[j] <= high;
         });
@@ -311,10 +315,7 @@ struct Words {
         if ((threadIdx.x & 63) == 63) at = atomicAdd(n, all);
         at = __builtin_amdgcn_readlane(at, 63) + upto - mine;
         fours(scale.alike, [&](int i, const float (&z)[4]) {
-            bool any = false;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) any |= z[j] >= low && z[j] <= high;
-            if (!any) return;
+            if (!__any(fmaxf(fmaxf(z[0], z[1]), fmaxf(z[2], z[3])) >= low)) return;
 #pragma unroll
             for (int j = 0; j < 4; ++j)
                 if (z[j] >= low && z[j] <= high) {
@@ -346,65 +347,64 @@ enum Kind { kCount, kWeight, kDraw };        // top_k: words, by place.  top_p: 
 // `over(f)` calls f(words) for the words of a source (registers, a list, memory), the same number of times in all lanes of a wave.
 template <int THREADS, int BINS, int LIST>
 struct Search {
-    static constexpr int kPerThread = BINS / THREADS, WAVES = THREADS / 64;
+    static constexpr int WAVES = THREADS / 64;
     Shared<BINS, LIST> &sh;
     const Scale &scale;
     u64 border;                              // place of the last word kept (0: all)
     uint32_t id_from;                        // ids go to bins from here on
-    int id_shift;
-    __device__ Search(Shared<BINS, LIST> &sh, const Scale &scale, uint32_t from, int n) : sh(sh), scale(scale), border(0), id_from(from), id_shift(0) {
+    int id_shift, coarse;                    // 2^coarse of the scale's bins are one here: a list needs few, and they are cleared and added up for every limit
+    __device__ Search(Shared<BINS, LIST> &sh, const Scale &scale, uint32_t from, int n) : sh(sh), scale(scale), border(0), id_from(from), id_shift(0), coarse(0) {
         while ((n - 1) >> id_shift >= BINS) ++id_shift;
     }
+    __device__ __forceinline__ void coarsen(int to) { coarse = to; id_shift += to; }
+    __device__ __forceinline__ int last_bin() const { return (BINS >> coarse) - 1; }
     __device__ __forceinline__ bool kept(float z, uint32_t id) const { return z > -INFINITY && place(z, id) >= border; }
     __device__ __forceinline__ u64 weigh(Kind kind, float z) const {
         const u64 w = kind == kCount ? 1 : scale.weight(z);
         return kind == kDraw && w < scale.least ? 0 : w;
     }
-    __device__ __forceinline__ int bin_at(Kind kind, float z, uint32_t id) const { return kind == kDraw ? (int)((id - id_from) >> id_shift) : scale.bin_of(z); }
+    __device__ __forceinline__ int bin_at(Kind kind, float z, uint32_t id) const { return kind == kDraw ? (int)((id - id_from) >> id_shift) : scale.bin_of(z) >> coarse; }
     __device__ __forceinline__ u64 order(Kind kind, float z, uint32_t id) const { return kind == kDraw ? ~(u64)id : place(z, id); }
     // Histogram of the words kept.  (Whoever read the last one did so in front of a barrier.)
     template <typename O>
     __device__ __forceinline__ void histogram(Kind kind, O over) {
-        for (int i = threadIdx.x; i < BINS; i += THREADS) sh.weight[i] = 0;
+        for (int i = threadIdx.x; i < BINS >> coarse; i += THREADS) sh.weight[i] = 0;
         __syncthreads();
         if (kind != kCount) over([&](auto some) {
 #pragma unroll
             for (int j = 0; j < some.M; ++j) {
                 u64 w = scale.weight(some.z[j]);
                 w = kept(some.z[j], some.id[j]) && !(kind == kDraw && w < scale.least) ? w : 0;
-                if (w) atomicAdd(&sh.weight[bin_at(kind, some.z[j], some.id[j])], w);
+                if (w) atomicAdd(&sh.weight[slot(bin_at(kind, some.z[j], some.id[j]))], w);
             }
         });
         else over([&](auto some) {
 #pragma unroll
             for (int j = 0; j < some.M; ++j)
-                if (kept(some.z[j], some.id[j])) atomicAdd(&sh.count[scale.bin_of(some.z[j])], 1);
+                if (kept(some.z[j], some.id[j])) atomicAdd(&sh.count[slot(bin_at(kCount, some.z[j], some.id[j]))], 1);
         });
         __syncthreads();
     }
     // The bin where want_of(all of the histogram) is reached from the front (the last one if it is not), and what is still wanted of that bin.
     template <typename F>
     __device__ __forceinline__ int find_bin(bool counts, u64 &want, u64 &total, F want_of) {
-        const int tid = threadIdx.x;
-        u64 h[kPerThread], sum = 0;
-#pragma unroll
-        for (int i = 0; i < kPerThread; ++i) {
-            h[i] = counts ? (u64)sh.count[tid * kPerThread + i] : sh.weight[tid * kPerThread + i];
-            sum += h[i];
-        }
+        const int tid = threadIdx.x, bins = BINS >> coarse, per_thread = (bins + THREADS - 1) / THREADS;
+        auto in_bin = [&](int i) { return counts ? (u64)sh.count[slot(tid * per_thread + i)] : sh.weight[slot(tid * per_thread + i)]; };
+        u64 sum = 0;
+#pragma unroll 4
+        for (int i = 0; i < per_thread; ++i) sum += in_bin(i);
         u64 upto = block_scan64<THREADS>(sum, sh, total) - sum;
         want = want_of(total);
         if (tid == 0) {
             sh.n = 0;                                         // of the bin's words, for resolve()
             sh.border = border;
-            if (total < want) { sh.bin = BINS - 1; sh.want = want; }
+            if (total < want) { sh.bin = bins - 1; sh.want = want; }
         }
         if (upto < want && upto + sum >= want) {
-#pragma unroll
-            for (int i = 0; i < kPerThread; ++i) {
-                if (upto < want && upto + h[i] >= want) { sh.bin = tid * kPerThread + i; sh.want = want - upto; }
-                upto += h[i];
-            }
+            int i = 0;
+            for (u64 h = in_bin(0); upto + h < want; h = in_bin(++i)) upto += h;
+            sh.bin = tid * per_thread + i;
+            sh.want = want - upto;
         }
         __syncthreads();
         want = uniform(sh.want);
@@ -415,7 +415,7 @@ struct Search {
     __device__ __forceinline__ void resolve(Kind kind, int bin, u64 want, O over) {
         const int tid = threadIdx.x, lane = tid & 63;
         u64 low = 0, high = ~0ull;                            // of the orders
-        const float low_z = kind == kDraw ? -INFINITY : scale.lowest(bin), high_z = kind == kDraw ? INFINITY : scale.highest(bin);
+        const float low_z = kind == kDraw ? -INFINITY : scale.lowest(((bin + 1) << coarse) - 1), high_z = kind == kDraw ? INFINITY : scale.highest(bin << coarse);
         auto inside = [&](float z, uint32_t id) {
             const u64 o = order(kind, z, id);
             return bin_at(kind, z, id) == bin && kept(z, id) && o >= low && o <= high;
@@ -424,7 +424,12 @@ struct Search {
         auto insiders = [&](auto f) {
             over([&](auto some) {
                 constexpr int M = decltype(some)::M;
-                bool any = false;                             // (most batches have no word of one bin)
+                // most batches have no word of one bin, and of those most none as large
+                float largest = some.z[0];
+#pragma unroll
+                for (int j = 1; j < M; ++j) largest = fmaxf(largest, some.z[j]);
+                if (!__any(largest >= low_z)) return;
+                bool any = false;
 #pragma unroll
                 for (int j = 0; j < M; ++j) any |= kind == kDraw ? bin_at(kind, some.z[j], some.id[j]) == bin : some.z[j] >= low_z && some.z[j] <= high_z;
                 if (!__any(any)) return;
@@ -453,7 +458,9 @@ struct Search {
                 if (tid < some) {
                     const u64 o = sh.small[tid], w = sh.small_w[tid];
                     u64 before = 0;
-                    for (int j = 0; j < some; ++j) before += sh.small[j] > o ? sh.small_w[j] : 0;
+                    for (int j0 = 0; j0 < some; j0 += 8)      // (eight from LDS at a time; kSmall is a multiple)
+#pragma unroll
+                        for (int j = j0; j < j0 + 8; ++j) before += j < some && sh.small[j] > o ? sh.small_w[j] : 0;
                     if (before < want && before + w >= want) { sh.border = o; sh.found_w = w; sh.word = (int)id_of(o); }
                 }
                 __syncthreads();
@@ -467,7 +474,7 @@ struct Search {
                 most_o = h > most_o ? h : most_o;
             }
             if (lane == 0) { sh.low64[tid >> 6] = least_o; sh.high64[tid >> 6] = most_o; }
-            for (int i = tid; i < BINS; i += THREADS) sh.weight[i] = 0;
+            for (int i = tid; i < BINS >> coarse; i += THREADS) sh.weight[i] = 0;
             __syncthreads();
             low = ~0ull;
             high = 0;
@@ -478,12 +485,12 @@ struct Search {
             low = uniform(low);
             high = uniform(high);
             int shift = 0;
-            while ((high - low) >> shift >= (u64)BINS) ++shift;
+            while ((high - low) >> shift >= (u64)(BINS >> coarse)) ++shift;
             insiders([&](bool is, float z, uint32_t id) {
                 if (!is) return;
                 const int at = (int)((high - order(kind, z, id)) >> shift);
-                if (kind == kCount) atomicAdd(&sh.count[at], 1);
-                else atomicAdd(&sh.weight[at], weigh(kind, z));
+                if (kind == kCount) atomicAdd(&sh.count[slot(at)], 1);
+                else atomicAdd(&sh.weight[slot(at)], weigh(kind, z));
             });
             __syncthreads();
             u64 total;
@@ -499,7 +506,7 @@ struct Search {
         histogram(kind, over);
         u64 want, total;
         const int bin = find_bin(kind == kCount, want, total, [&](u64 all) { return kind == kCount ? (u64)l.k : kind == kWeight ? l.want_p(all) : l.target(all) + 1; });
-        if (bin < BINS - 1 || kind == kDraw) resolve(kind, bin, want, over);      // in the last bin nothing has a weight
+        if (bin < last_bin() || kind == kDraw) resolve(kind, bin, want, over);      // in the last bin nothing has a weight
         return total;
     }
     // All limits and the draw.
@@ -586,11 +593,14 @@ __device__ __forceinline__ u64 draw_from_registers(const W &words, S &sh, const 
     return total;
 }
 
+template <typename Z, int THREADS, int R>
+constexpr int row_bins() { return bins_of(THREADS * R * Row<Z>::E); }
 // A row in the registers of one workgroup.
 template <typename Z, int THREADS, int R>
 __global__ __launch_bounds__(THREADS, 4) void sample_row_kernel(SampleArgs a, int bits) {
-    constexpr int BINS = bins_of(THREADS), LIST = list_of(THREADS);
-    __shared__ Shared<BINS, LIST> sh;
+    constexpr int BINS = row_bins<Z, THREADS, R>(), LIST = list_of(THREADS * R * Row<Z>::E);
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    Shared<BINS, LIST> &sh = *reinterpret_cast<Shared<BINS, LIST> *>(lds);
     const int tid = threadIdx.x, n = blockIdx.x, V = a.V;
     const Limits l(a, n);
     const Words<Z, THREADS, R> words(static_cast<const Z *>(a.logits) + n * a.ld, V);
@@ -619,7 +629,7 @@ __global__ __launch_bounds__(THREADS, 4) void sample_row_kernel(SampleArgs a, in
     bool in_list = false;
     int listed = 0;
     if (l.few(V) && l.k <= THREADS / 2) {
-        if (mine > -INFINITY) atomicAdd(&sh.count[scale.bin_of(mine)], 1);
+        if (mine > -INFINITY) atomicAdd(&sh.count[slot(scale.bin_of(mine))], 1);
         __syncthreads();
         u64 want, all;
         const int edge = search.find_bin(true, want, all, [&](u64) { return (u64)l.k; });
@@ -628,6 +638,7 @@ __global__ __launch_bounds__(THREADS, 4) void sample_row_kernel(SampleArgs a, in
             __syncthreads();
             listed = __builtin_amdgcn_readfirstlane(sh.n);
             in_list = listed <= LIST;
+            if (in_list) search.coarsen(BINS > THREADS ? __builtin_ctz(BINS / THREADS) : 0);
         }
     }
     auto over = [&](auto f) {
@@ -896,21 +907,29 @@ __global__ __launch_bounds__(kPickThreads, 4) void sample_pick_kernel(SampleArgs
 template <typename Z>
 int segments_of(int V) { return (V + segment_words<Z>() - 1) / segment_words<Z>(); }
 
+template <typename Z, int THREADS, int R>
+hipError_t launch_row(const SampleArgs &a, int bits, hipStream_t stream) {
+    static LdsLimit limit;
+    constexpr size_t bytes = sizeof(Shared<row_bins<Z, THREADS, R>(), list_of(THREADS * R * Row<Z>::E)>);
+    const auto kernel = sample_row_kernel<Z, THREADS, R>;
+    const hipError_t e = limit.ensure(reinterpret_cast<const void *>(kernel), bytes);
+    if (e != hipSuccess) return e;
+    kernel<<<a.N, THREADS, bytes, stream>>>(a, bits);
+    return hipGetLastError();
+}
 template <typename Z>
 hipError_t launch(const SampleArgs &a, int bits, hipStream_t stream) {
     const int vectors = (a.V + Row<Z>::E - 1) / Row<Z>::E;
-    if (vectors <= 256 * 4) sample_row_kernel<Z, 256, 4><<<a.N, 256, 0, stream>>>(a, bits);
-    else if (vectors <= 1024 * 4) sample_row_kernel<Z, 1024, 4><<<a.N, 1024, 0, stream>>>(a, bits);
-    else if (vectors <= 1024 * 16) sample_row_kernel<Z, 1024, 16><<<a.N, 1024, 0, stream>>>(a, bits);
-    else {
-        const int segments = segments_of<Z>(a.V);
-        if ((long long)a.N * segments > 0x7FFFFFFF) return hipErrorInvalidValue;
-        const int groups = a.N * segments;
-        sample_tops_kernel<Z><<<groups, kSegThreads, 0, stream>>>(a, segments);
-        sample_weigh_kernel<Z><<<groups, kSegThreads, 0, stream>>>(a, segments, bits);
-        sample_gather_kernel<Z><<<groups, kSegThreads, 0, stream>>>(a, segments, bits);
-        sample_pick_kernel<Z><<<a.N, kPickThreads, 0, stream>>>(a, segments, bits);
-    }
+    if (vectors <= 256 * 4) return launch_row<Z, 256, 4>(a, bits, stream);
+    if (vectors <= 1024 * 4) return launch_row<Z, 1024, 4>(a, bits, stream);
+    if (vectors <= 1024 * 16) return launch_row<Z, 1024, 16>(a, bits, stream);
+    const int segments = segments_of<Z>(a.V);
+    if ((long long)a.N * segments > 0x7FFFFFFF) return hipErrorInvalidValue;
+    const int groups = a.N * segments;
+    sample_tops_kernel<Z><<<groups, kSegThreads, 0, stream>>>(a, segments);
+    sample_weigh_kernel<Z><<<groups, kSegThreads, 0, stream>>>(a, segments, bits);
+    sample_gather_kernel<Z><<<groups, kSegThreads, 0, stream>>>(a, segments, bits);
+    sample_pick_kernel<Z><<<a.N, kPickThreads, 0, stream>>>(a, segments, bits);
     return hipGetLastError();
 }
 
