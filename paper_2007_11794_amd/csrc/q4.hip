@@ -23,17 +23,46 @@ constexpr size_t kLdsRows = 144 * 1024;                      // most LDS for the
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef u32x4 u32x4_any __attribute__((aligned(1)));         // rows of codes may start anywhere
 
-__device__ __forceinline__ float row_element(const void *x, long long i, bool bf16) {
-    return bf16 ? bf16_to_f32(static_cast<const uint16_t *>(x)[i]) : static_cast<const float *>(x)[i];
+typedef f32x4 f32x4_any __attribute__((aligned(4)));
+typedef uint64_t u64_any __attribute__((aligned(2)));
+typedef uint32_t u32_any __attribute__((aligned(1)));
+typedef uint16_t u16_any __attribute__((aligned(1)));
+
+// Elements k .. k + 7 of a row of H, 0 behind it.
+__device__ __forceinline__ void eight_of_row(const void *x, long long at, int k, int H, bool bf16, float (&out)[8]) {
+    if (k + 8 <= H) {
+        if (bf16) {
+            const u32x4 v = *reinterpret_cast<const u32x4_any *>(static_cast<const uint16_t *>(x) + at + k);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) { out[2 * i] = __uint_as_float(v[i] << 16); out[2 * i + 1] = __uint_as_float(v[i] & 0xFFFF0000u); }
+        } else {
+            const float *p = static_cast<const float *>(x) + at + k;
+            const f32x4 a = *reinterpret_cast<const f32x4_any *>(p), b = *reinterpret_cast<const f32x4_any *>(p + 4);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) { out[i] = a[i]; out[4 + i] = b[i]; }
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            out[i] = k + i >= H ? 0.f : bf16 ? bf16_to_f32(static_cast<const uint16_t *>(x)[at + k + i]) : static_cast<const float *>(x)[at + k + i];
+    }
 }
 
-// What a wave needs of one step of one tile of 16 words.
-template <int GROUPS>
+// What a wave needs of one step of NT tiles of 16 words, as it comes from memory.
+template <int NT, int GROUPS, bool ZERO>
 struct Codes {
-    u32x4 w;
-    uint32_t scale[GROUPS], zero[GROUPS];
+    u32x4 w[NT];
+    uint64_t scale[GROUPS];              // NT of them, of either type
+    uint32_t zero[ZERO ? GROUPS : 1];
+    float bias[NT];                      // with the last step of a tile: a load behind the requests of later steps would have to wait for them
 };
 
+// (w & mask) | exponents in one instruction (of two literals it takes none, and the compiler makes two)
+__device__ __forceinline__ uint32_t and_or(uint32_t w, uint32_t mask, uint32_t exponents) {
+    uint32_t r;
+    asm("v_and_or_b32 %0, %1, %2, %3" : "=v"(r) : "v"(w), "s"(mask), "v"(exponents));
+    return r;
+}
 // Eight codes of a dword less their zero, as fp16 in the order 0 4 1 5 2 6 3 7 (the rows are staged in that order too).  A code under
 // the exponent of 1024 (of 64, four bits further up) is 1024 (64) more than itself; less1024 is -(1024 + zero), less64 -(64 + zero).
 __device__ __forceinline__ f16x8 eight_codes(uint32_t w, f16x2 less1024, f16x2 less64) {
@@ -41,172 +70,269 @@ __device__ __forceinline__ f16x8 eight_codes(uint32_t w, f16x2 less1024, f16x2 l
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         const uint32_t s = w >> (8 * i);
-        p[2 * i] = __builtin_bit_cast(f16x2, (s & 0x000F000Fu) | 0x64006400u) + less1024;
-        p[2 * i + 1] = __builtin_bit_cast(f16x2, (s & 0x00F000F0u) | 0x54005400u) + less64;
+        p[2 * i] = __builtin_bit_cast(f16x2, and_or(s, 0x000F000Fu, 0x64006400u)) + less1024;
+        p[2 * i + 1] = __builtin_bit_cast(f16x2, and_or(s, 0x00F000F0u, 0x54005400u)) + less64;
     }
     return f16x8{p[0][0], p[0][1], p[1][0], p[1][1], p[2][0], p[2][1], p[3][0], p[3][1]};
 }
 
 // dword i of the lanes 16 j + c goes to dword j of the lanes 16 i + c
-__device__ __forceinline__ void transpose4(u32x4 &w) {
+__device__ __forceinline__ u32x4 transposed(u32x4 w) {
     auto a = __builtin_amdgcn_permlane32_swap(w[0], w[2], false, false);
     auto b = __builtin_amdgcn_permlane32_swap(w[1], w[3], false, false);
     auto c = __builtin_amdgcn_permlane16_swap(a[0], b[0], false, false);
     auto d = __builtin_amdgcn_permlane16_swap(a[1], b[1], false, false);
-    w = u32x4{c[0], c[1], d[0], d[1]};
+    return u32x4{c[0], c[1], d[0], d[1]};
+}
+
+// w without its first n bytes (the rest is of no account)
+__device__ __forceinline__ u32x4 without(u32x4 w, uint32_t n) {
+    const uint64_t lo = (uint64_t)w[1] << 32 | w[0], hi = (uint64_t)w[3] << 32 | w[2];
+    const uint32_t bits = 8 * (n & 7);
+    const uint64_t a = n & 8 ? hi : lo, b = n & 8 ? 0 : hi;
+    const uint64_t x = n >= 16 ? 0 : bits ? a >> bits | b << (64 - bits) : a, y = n >= 16 ? 0 : b >> bits;
+    return u32x4{(uint32_t)x, (uint32_t)(x >> 32), (uint32_t)y, (uint32_t)(y >> 32)};
 }
 
 template <int TERMS, int MT, int NT, int G, bool ZERO>
-__global__ __launch_bounds__(kThreads, 4) void q4_kernel(Q4Args a, int chunk, int rounds) {
+__global__ __launch_bounds__(kThreads, 4) void q4_kernel(Q4Args a, int chunk_steps, int rounds) {
     constexpr int kRows = 16 * MT, kGroups = kStep / G;
-    extern __shared__ __attribute__((aligned(1024))) char lds[];        // [chunk / 32][MT][TERMS][64 lanes][8]
-    __shared__ int row_exp[kRows];                                      // power of two that the row was divided by
+    extern __shared__ __attribute__((aligned(1024))) char lds[];        // [units of a chunk / 32][MT][TERMS][64 lanes][8]
+    __shared__ uint32_t row_top[kRows];                                 // the row's largest finite magnitude
+    __shared__ int row_exp[kRows];                                      // the power of two that it is divided by
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 15, g = lane >> 4;
     const int r0 = blockIdx.y * kRows, rows = a.B - r0 < kRows ? a.B - r0 : kRows;
-    const int row_bytes = (a.H + 1) >> 1, Hp = (a.H + kStep - 1) / kStep * kStep, last_group = (a.H + G - 1) / G - 1;
-    const uint8_t *const end = a.codes + (long long)(a.V - 1) * a.code_ld + row_bytes;
+    const int steps = (a.H + kStep - 1) / kStep, last_group = (a.H + G - 1) / G - 1, stride = gridDim.x * kWaves;
+    const int tiles = (a.V + 16 * NT - 1) / (16 * NT), scale_size = a.scale_bf16 ? 2 : 4;
+    const uint8_t *const end = a.codes + (long long)(a.V - 1) * a.code_ld + ((a.H + 1) >> 1), *const last = end - 16;
 
-    auto request = [&](int tile, int step, Codes<kGroups> (&q)[NT]) {
+    // Tiles from here on may have loads that pass the end of the codes: a lane's last one ends up to 63 bytes behind its row.
+    const int clear = (a.V - 64) / (16 * NT);
+    // Requests run two steps ahead of the products, over the ends of tiles.
+    int tile_r = blockIdx.x * kWaves + wave, step_r = 0;
+    const uint8_t *word_r[NT];
+    uint32_t v_r;                                                       // first word of a lane, in the array whatever the tile
+    auto set_tile = [&]() {
+        const int v = tile_r * 16 * NT + NT * c, top = a.V - NT;        // (two words of a lane: V > 1)
+        v_r = (uint32_t)(v < top ? v : top);
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            int v = (tile * NT + n) * 16 + c;
-            if (v >= a.V) v = a.V - 1;
-            const int off = step * (kStep / 2) + 16 * g;
-            const uint8_t *p = a.codes + v * a.code_ld + off;
-            q[n].w = u32x4{0, 0, 0, 0};
-            if (off < row_bytes) {                                      // behind a row come the next one's bytes, times zeros
-                if (p + 16 <= end) q[n].w = *reinterpret_cast<const u32x4_any *>(p);
-                else
-                    for (int i = 0; i < 16; ++i)
-                        if (p + i < end) q[n].w[i >> 2] |= (uint32_t)p[i] << (8 * (i & 3));
+        for (int n = 0; n < NT; ++n) word_r[n] = a.codes + (long long)(v + n < a.V ? v + n : a.V - 1) * a.code_ld + 16 * g;
+    };
+    auto request = [&](Codes<NT, kGroups, ZERO> &q) {
+        if (tile_r < tiles) {
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                const uint8_t *p = word_r[n] + step_r * (kStep / 2);
+                if (tile_r < clear) {                                   // behind a row come the next one's bytes, times zeros
+                    q.w[n] = *reinterpret_cast<const u32x4_any *>(p);
+                } else if (last >= a.codes) {                           // the codes end: from further in front, see beyond()
+                    q.w[n] = *reinterpret_cast<const u32x4_any *>(p > last ? last : p);
+                } else {                                                // less than 16 bytes of codes in all
+                    uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll 1
+                    for (int i = 0; i < 16 && p + i < end; ++i) {
+                        const uint32_t byte = (uint32_t)p[i] << (8 * (i & 3));
+#pragma unroll
+                        for (int d = 0; d < 4; ++d) w[d] |= i >> 2 == d ? byte : 0;
+                    }
+                    q.w[n] = u32x4{w[0], w[1], w[2], w[3]};
+                }
             }
 #pragma unroll
             for (int i = 0; i < kGroups; ++i) {
-                int grp = step * kGroups + i;
-                if (grp > last_group) grp = last_group;
-                const long long at = (long long)grp * a.V + v;
-                q[n].scale[i] = a.scale_bf16 ? (uint32_t)static_cast<const uint16_t *>(a.scale)[at] << 16 : static_cast<const uint32_t *>(a.scale)[at];
-                q[n].zero[i] = ZERO ? a.zero[at] : 0;
+                const int grp = step_r * kGroups + i < last_group ? step_r * kGroups + i : last_group;
+                const char *s = static_cast<const char *>(a.scale) + (long long)grp * a.V * scale_size;
+                if (a.scale_bf16) {
+                    if (NT == 2) q.scale[i] = *reinterpret_cast<const u32_any *>(s + v_r * 2u);
+                    else q.scale[i] = *reinterpret_cast<const uint16_t *>(s + v_r * 2u);
+                } else {
+                    if (NT == 2) q.scale[i] = *reinterpret_cast<const u64_any *>(s + v_r * 4u);
+                    else q.scale[i] = *reinterpret_cast<const uint32_t *>(s + v_r * 4u);
+                }
+                if (ZERO) {                                            
+                    const uint8_t *z = a.zero + (long long)grp * a.V;
+                    if (NT == 2) q.zero[i] = *reinterpret_cast<const u16_any *>(z + v_r);
+                    else q.zero[i] = z[v_r];
+                }
             }
+            if (step_r + 1 == steps)
+#pragma unroll
+                for (int n = 0; n < NT; ++n) q.bias[n] = a.bias ? a.bias[v_r + n] : 0.f;
+        }
+        if (++step_r == steps) {
+            step_r = 0;
+            tile_r += stride;
+            set_tile();
         }
     };
 
-    const int tiles = (a.V + 16 * NT - 1) / (16 * NT);
-    int tile = blockIdx.x * kWaves + wave;
-    Codes<kGroups> q[NT];
-    if (tile < tiles) request(tile, 0, q);                              // on their way while the rows are staged
+    set_tile();
+    Codes<NT, kGroups, ZERO> q[3];
+    request(q[0]);
+    request(q[1]);                                                      // on their way while the rows are staged
 
-    // the power of two of every row: its largest finite magnitude goes to [2^14, 2^15)
-    for (int r = wave; r < kRows; r += kWaves) {
-        float top = 0.f;
-        if (r < rows)
-            for (int j = lane; j < a.H; j += 64) {
-                const float m = fabsf(row_element(a.x, (r0 + r) * a.x_ld + j, a.x_bf16));
-                if (m < INFINITY) top = fmaxf(top, m);
-            }
-        top = wave_max(top);
-        if (lane == 0) row_exp[r] = top > 0.f ? ilogbf(top) - 14 : 0;
+    // The power of two of every row: its largest finite magnitude goes to [2^14, 2^15).
+    for (int r = tid; r < kRows; r += kThreads) row_top[r] = 0;
+    __syncthreads();
+    for (int i = tid; i < kRows * steps * 16; i += kThreads) {
+        const int r = i % kRows, k = i / kRows * 8;
+        if (r >= rows || k >= a.H) continue;
+        float x[8];
+        eight_of_row(a.x, (r0 + r) * a.x_ld, k, a.H, a.x_bf16, x);
+        uint32_t top = 0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const uint32_t m = __float_as_uint(x[j]) & 0x7FFFFFFFu;
+            if (m < 0x7F800000u && m > top) top = m;
+        }
+        atomicMax(&row_top[r], top);
     }
     __syncthreads();
+    for (int r = tid; r < kRows; r += kThreads) row_exp[r] = row_top[r] ? ilogbf(__uint_as_float(row_top[r])) - 14 : 0;
+    __syncthreads();
+    // First unit of lane group g in product t of 32 units: as the codes are where a step is one group, else with the codes transposed.
+    auto unit_of = [](int t, int g) { return G == kStep ? t / 4 * kStep + 32 * g + t % 4 * 8 : 32 * t + 8 * g; };
     auto stage = [&](int k0, int n) {                                   // units k0 .. k0 + n - 1
         for (int i = tid; i < n / 32 * MT * 64; i += kThreads) {
-            const int frag = i >> 6, l = i & 63, r = (frag % MT) * 16 + (l & 15), k = k0 + frag / MT * 32 + (l >> 4) * 8, e = row_exp[r];
+            const int frag = i >> 6, l = i & 63, r = (frag % MT) * 16 + (l & 15), k = k0 + unit_of(frag / MT, l >> 4);
+            float x[8] = {};
+            if (r < rows) eight_of_row(a.x, (r0 + r) * a.x_ld, k, a.H, a.x_bf16, x);
+            const int e = row_exp[r];
             f16x8 t1, t2;
 #pragma unroll
             for (int s = 0; s < 8; ++s) {
-                const int j = k + (s >> 1) + 4 * (s & 1);
-                const float x = r < rows && j < a.H ? ldexpf(row_element(a.x, (r0 + r) * a.x_ld + j, a.x_bf16), -e) : 0.f;
-                t1[s] = (_Float16)x;
-                t2[s] = (_Float16)(fabsf(x) < INFINITY ? x - (float)t1[s] : 0.f);       // (a NaN is in the first term)
+                const float y = ldexpf(x[(s >> 1) + 4 * (s & 1)], -e);
+                t1[s] = (_Float16)y;
+                t2[s] = (_Float16)(fabsf(y) < INFINITY ? y - (float)t1[s] : 0.f);       // (a NaN is in the first term)
             }
             *reinterpret_cast<f16x8 *>(lds + (size_t)frag * TERMS * 1024 + l * 16) = t1;
             if (TERMS == 2) *reinterpret_cast<f16x8 *>(lds + (size_t)frag * 2048 + 1024 + l * 16) = t2;
         }
     };
 
-    for (int round = 0; round < rounds; ++round, tile += gridDim.x * kWaves) {
-        f32x4 acc[MT][NT];
+    f32x4 acc[MT][NT];
+    int tile = blockIdx.x * kWaves + wave, step = 0, left = rounds * steps, in_chunk = 0;
+    bool staged = false;
+    auto body = [&](Codes<NT, kGroups, ZERO> &now, Codes<NT, kGroups, ZERO> &free) {
+        if (in_chunk == 0 && !(staged && chunk_steps >= steps)) {       // (the same in all waves)
+            if (staged) __syncthreads();                                // the chunk before has been read
+            const int n = steps - step < chunk_steps ? steps - step : chunk_steps;
+            stage(step * kStep, n * kStep);
+            staged = true;
+            __syncthreads();
+        }
+        request(free);
+        if (tile < tiles) {
+            if (step == 0)
 #pragma unroll
-        for (int m = 0; m < MT; ++m)
+                for (int m = 0; m < MT; ++m)
 #pragma unroll
-            for (int n = 0; n < NT; ++n) acc[m][n] = f32x4{0.f, 0.f, 0.f, 0.f};
-        for (int k0 = 0; k0 < Hp; k0 += chunk) {
-            const int now = Hp - k0 < chunk ? Hp - k0 : chunk;
-            if (round == 0 || chunk < Hp) {
-                if (round || k0) __syncthreads();                       // the chunk before has been read
-                stage(k0, now);
-                __syncthreads();
+                    for (int n = 0; n < NT; ++n) acc[m][n] = f32x4{0.f, 0.f, 0.f, 0.f};
+            const int v = tile * 16 * NT + NT * c;
+            bool edge = false;
+            u32x4 w[NT];
+#pragma unroll
+            for (int n = 0; n < NT; ++n) w[n] = now.w[n];
+            if (tile >= clear) {
+                // loads that began too early, and a lane's one word that was loaded as the second of two
+                edge = NT == 2 && v + 2 > a.V;
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    const uint8_t *p = a.codes + (long long)(v + n < a.V ? v + n : a.V - 1) * a.code_ld + 16 * g + step * (kStep / 2);
+                    if (last >= a.codes && p > last) w[n] = without(w[n], p - last < 16 ? (uint32_t)(p - last) : 16u);
+                }
+                if (edge) {
+#pragma unroll
+                    for (int i = 0; i < kGroups; ++i) {
+                        now.scale[i] >>= a.scale_bf16 ? 16 : 32;
+                        if (ZERO) now.zero[i] >>= 8;
+                    }
+                    now.bias[0] = now.bias[NT - 1];
+                }
             }
-            if (tile >= tiles) continue;
-            for (int k = 0; k < now; k += kStep) {
-                Codes<kGroups> cur[NT];
+            if (G != kStep)
 #pragma unroll
-                for (int n = 0; n < NT; ++n) cur[n] = q[n];
-                const bool row_ends = k0 + k + kStep >= Hp;
-                const int next = row_ends ? tile + (int)gridDim.x * kWaves : tile;
-                if (next < tiles) request(next, row_ends ? 0 : (k0 + k) / kStep + 1, q);
-                f32x4 part[MT][NT];
+                for (int n = 0; n < NT; ++n) w[n] = transposed(w[n]);
+            f32x4 part[MT][NT];
 #pragma unroll
-                for (int n = 0; n < NT; ++n) transpose4(cur[n].w);
+            for (int t = 0; t < 4; ++t) {                               // 32 units each
+                constexpr int kPer = G / 32;
+                const int grp = t / kPer;
+                f16x8 b[NT];
 #pragma unroll
-                for (int t = 0; t < 4; ++t) {                           // 32 units each
-                    const int grp = t * 32 / G;
-                    f16x8 b[NT];
+                for (int n = 0; n < NT; ++n) {
+                    uint32_t z = 8u;
+                    if (ZERO) z = NT == 1 ? now.zero[grp] : n == 1 ? now.zero[grp] >> 8 : now.zero[grp] & 255u;
+                    const f16x2 less = __builtin_bit_cast(f16x2, 0xE400E400u | z * 0x00010001u);
+                    b[n] = eight_codes(w[n][t], less, less + f16x2{(_Float16)960.f, (_Float16)960.f});
+                }
+#pragma unroll
+                for (int m = 0; m < MT; ++m) {
+                    const char *at = lds + (size_t)((in_chunk * 4 + t) * MT + m) * TERMS * 1024 + lane * 16;
+                    const f16x8 x1 = *reinterpret_cast<const f16x8 *>(at);
+                    f16x8 x2;
+                    if (TERMS == 2) x2 = *reinterpret_cast<const f16x8 *>(at + 1024);
 #pragma unroll
                     for (int n = 0; n < NT; ++n) {
-                        const uint32_t z = ZERO ? cur[n].zero[grp] : 8u;
-                        const f16x2 less = __builtin_bit_cast(f16x2, 0xE400E400u | z * 0x00010001u);
-                        b[n] = eight_codes(cur[n].w[t], less, less + f16x2{(_Float16)960.f, (_Float16)960.f});
-                    }
-#pragma unroll
-                    for (int m = 0; m < MT; ++m) {
-                        const char *at = lds + (size_t)((k / 32 + t) * MT + m) * TERMS * 1024 + lane * 16;
-                        const f16x8 x1 = *reinterpret_cast<const f16x8 *>(at);
-                        f16x8 x2;
-                        if (TERMS == 2) x2 = *reinterpret_cast<const f16x8 *>(at + 1024);
-#pragma unroll
-                        for (int n = 0; n < NT; ++n) {
-                            if (t * 32 % G == 0) part[m][n] = f32x4{0.f, 0.f, 0.f, 0.f};
-                            if (TERMS == 2) part[m][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x2, b[n], part[m][n], 0, 0, 0);
-                            part[m][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x1, b[n], part[m][n], 0, 0, 0);
-                            if ((t + 1) * 32 % G == 0) {
-                                const float s = __uint_as_float(cur[n].scale[grp]);
-#pragma unroll
-                                for (int i = 0; i < 4; ++i) acc[m][n][i] = __builtin_fmaf(s, part[m][n][i], acc[m][n][i]);
-                            }
-                        }
+                        if (t % kPer == 0) part[m][n] = f32x4{0.f, 0.f, 0.f, 0.f};
+                        if (TERMS == 2) part[m][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x2, b[n], part[m][n], 0, 0, 0);
+                        part[m][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x1, b[n], part[m][n], 0, 0, 0);
                     }
                 }
+                if (t % kPer == kPer - 1)
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                        const uint64_t raw = now.scale[grp];
+                        constexpr bool kPair = NT == 2;
+                        const bool second = kPair && n == 1;
+                        const uint32_t bits = a.scale_bf16 ? (second ? (uint32_t)raw & 0xFFFF0000u : (uint32_t)raw << 16) : (second ? (uint32_t)(raw >> 32) : (uint32_t)raw);
+                        const float s = __uint_as_float(bits);
+#pragma unroll
+                        for (int m = 0; m < MT; ++m)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) acc[m][n][i] = __builtin_fmaf(s, part[m][n][i], acc[m][n][i]);
+                    }
+            }
+            if (step + 1 == steps && v < a.V) {
+#pragma unroll
+                for (int m = 0; m < MT; ++m)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int r = m * 16 + 4 * g + i;
+                        if (r >= rows) continue;
+                        const int e = row_exp[r];
+                        float y[NT];
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) y[n] = ldexpf(acc[m][n][i], e) + now.bias[n];
+                        const long long at = (r0 + r) * a.y_ld + v;
+                        if (NT == 2 && !edge) {
+                            if (a.y_bf16) *reinterpret_cast<u32_any *>(static_cast<uint16_t *>(a.y) + at) = pack_bf16x2(y[0], y[NT - 1]);
+                            else *reinterpret_cast<u64_any *>(static_cast<float *>(a.y) + at) = (uint64_t)__float_as_uint(y[NT - 1]) << 32 | __float_as_uint(y[0]);
+                        } else if (a.y_bf16) static_cast<uint16_t *>(a.y)[at] = (uint16_t)pack_bf16x2(y[0], 0.f);
+                        else static_cast<float *>(a.y)[at] = y[0];
+                    }
             }
         }
-        if (tile >= tiles) continue;
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            const int v = (tile * NT + n) * 16 + c;
-            if (v >= a.V) continue;
-            const float bias = a.bias ? a.bias[v] : 0.f;
-#pragma unroll
-            for (int m = 0; m < MT; ++m)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int r = m * 16 + 4 * g + i;
-                    if (r >= rows) continue;
-                    const float y = ldexpf(acc[m][n][i], row_exp[r]) + bias;
-                    const long long at = (r0 + r) * a.y_ld + v;
-                    if (a.y_bf16) static_cast<uint16_t *>(a.y)[at] = (uint16_t)pack_bf16x2(y, 0.f);
-                    else static_cast<float *>(a.y)[at] = y;
-                }
-        }
+        if (++in_chunk == chunk_steps) in_chunk = 0;
+        if (++step == steps) { step = in_chunk = 0; tile += stride; }
+    };
+    while (true) {                                                      // the three sets of codes in turn, so that none is ever copied
+        body(q[0], q[2]);
+        if (--left == 0) break;
+        body(q[1], q[0]);
+        if (--left == 0) break;
+        body(q[2], q[1]);
+        if (--left == 0) break;
     }
 }
 
 template <int TERMS, int MT, int NT, int G, bool ZERO>
 hipError_t launch(const Q4Args &a, hipStream_t stream) {
     static LdsLimit limit;
-    const int Hp = (a.H + kStep - 1) / kStep * kStep, unit = 16 * MT * 2 * TERMS;          // bytes of LDS per unit
-    int chunk = (int)(kLdsRows / unit) / kStep * kStep;
-    if (chunk > Hp) chunk = Hp;
-    const size_t bytes = (size_t)chunk * unit;
+    const int steps = (a.H + kStep - 1) / kStep, step_bytes = 16 * MT * 2 * TERMS * kStep;
+    int chunk = (int)(kLdsRows / step_bytes);
+    if (chunk > steps) chunk = steps;
+    const size_t bytes = (size_t)chunk * step_bytes;
     const auto kernel = q4_kernel<TERMS, MT, NT, G, ZERO>;
     const hipError_t e = limit.ensure(reinterpret_cast<const void *>(kernel), bytes);
     if (e != hipSuccess) return e;
@@ -227,22 +353,24 @@ hipError_t launch(const Q4Args &a, hipStream_t stream) {
     return hipGetLastError();
 }
 
-template <int TERMS, int MT, int NT>
+// Pairs of tiles where there are few rows, registers for them, and words enough that no wave goes without.
+template <int TERMS, int MT, int G, bool ZERO>
+hipError_t by_words(const Q4Args &a, hipStream_t stream) {
+    if constexpr (MT == 1 && G > 32)
+        if (a.V >= 32 * kWaves * kChipGroups) return launch<TERMS, MT, 2, G, ZERO>(a, stream);
+    return launch<TERMS, MT, 1, G, ZERO>(a, stream);
+}
+template <int TERMS, int MT>
 hipError_t by_group(const Q4Args &a, hipStream_t stream) {
     switch (a.group) {
-        case 32: return a.zero ? launch<TERMS, MT, NT, 32, true>(a, stream) : launch<TERMS, MT, NT, 32, false>(a, stream);
-        case 64: return a.zero ? launch<TERMS, MT, NT, 64, true>(a, stream) : launch<TERMS, MT, NT, 64, false>(a, stream);
-        default: return a.zero ? launch<TERMS, MT, NT, 128, true>(a, stream) : launch<TERMS, MT, NT, 128, false>(a, stream);
+        case 32: return a.zero ? by_words<TERMS, MT, 32, true>(a, stream) : by_words<TERMS, MT, 32, false>(a, stream);
+        case 64: return a.zero ? by_words<TERMS, MT, 64, true>(a, stream) : by_words<TERMS, MT, 64, false>(a, stream);
+        default: return a.zero ? by_words<TERMS, MT, 128, true>(a, stream) : by_words<TERMS, MT, 128, false>(a, stream);
     }
 }
-
 template <int TERMS>
 hipError_t by_rows(const Q4Args &a, hipStream_t stream) {
-    // Tiles of 16 words where pairs of them would leave waves without any.
-    const bool few_words = a.V < 32 * kWaves * kChipGroups;
-    if (a.B <= 16) return few_words ? by_group<TERMS, 1, 1>(a, stream) : by_group<TERMS, 1, 2>(a, stream);
-    if (a.B <= 32) return few_words ? by_group<TERMS, 2, 1>(a, stream) : by_group<TERMS, 2, 2>(a, stream);
-    return few_words ? by_group<TERMS, 4, 1>(a, stream) : by_group<TERMS, 4, 2>(a, stream);
+    return a.B <= 16 ? by_group<TERMS, 1>(a, stream) : a.B <= 32 ? by_group<TERMS, 2>(a, stream) : by_group<TERMS, 4>(a, stream);
 }
 
 }  // namespace
