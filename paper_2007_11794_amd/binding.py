@@ -528,36 +528,75 @@ def rnnlm_hs_time_query(model: RnnlmModel, query_word, h_out, logprob, repeats: 
     return ms.value
 
 
-def _rows(t, name, dtype=None):
-    """(pointer, stride of a row, rnnlm_dtype) of a device matrix whose rows are contiguous, in float32 or bfloat16."""
-    import torch
-    code = RNNLM_F32 if t.dtype == torch.float32 else RNNLM_BF16 if t.dtype == torch.bfloat16 else None
-    if t.dim() != 2 or not t.is_cuda or code is None or (t.shape[1] > 1 and t.stride(1) != 1) or (dtype is not None and t.dtype != dtype):
-        raise TypeError("%s must be a device matrix of contiguous rows in %s" % (name, dtype or "float32 or bfloat16"))
-    return t.data_ptr() or None, int(t.stride(0)) if t.shape[0] > 1 else max(int(t.stride(0)), int(t.shape[1])), code
+_torch_types = None
+
+
+def _types():
+    """(float32, bfloat16, uint8, int32) of torch, looked up once."""
+    global _torch_types
+    if _torch_types is None:
+        import torch
+        lib()
+        _torch_types = (torch.float32, torch.bfloat16, torch.uint8, torch.int32)
+    return _torch_types
+
+
+def _rows(t, shape, name):
+    """(pointer, stride of a row, rnnlm_dtype) of a device matrix of that shape whose rows are contiguous, in float32 or bfloat16."""
+    f32, bf16, _, _ = _torch_types
+    dtype = t.dtype
+    code = RNNLM_F32 if dtype is f32 else RNNLM_BF16 if dtype is bf16 else -1
+    if not t.is_cuda or code < 0 or len(shape) != 2:
+        raise TypeError("%s must be a device matrix of contiguous rows in float32 or bfloat16" % name)
+    ld, one = t.stride()
+    if one != 1 and shape[1] > 1:
+        raise TypeError("%s must be a device matrix of contiguous rows in float32 or bfloat16" % name)
+    return t.data_ptr() or None, ld if shape[0] > 1 and ld >= 0 else max(ld, shape[1]), code
+
+
+def _same(t, dtype, shape, name):
+    """Device pointer of a contiguous CUDA tensor of the given type and shape (None -> NULL)."""
+    if t is None:
+        return None
+    if t.shape != shape:
+        raise TypeError("shape mismatch")
+    if t.dtype is not dtype or not t.is_cuda or not t.is_contiguous():
+        raise TypeError("%s must be a contiguous device tensor of dtype %s" % (name, dtype))
+    return t.data_ptr() or None
+
+
+def _space(workspace):
+    """(pointer, bytes) of a workspace."""
+    if workspace is None:
+        return None, 0
+    return _dev(workspace, _torch_types[2], "workspace"), workspace.numel()
 
 
 def rnnlm_q4_matvec(codes, scales, group: int, x, y, zeros=None, bias=None, stream=None):
     """y [B,V] = rows of x [B,H] times 4-bit weights: codes uint8 [V, at least ceil(H / 2)] (row stride free), scales float32 or
     bfloat16 [ceil(H / group), V], zeros uint8 of the same shape or None (8 everywhere), bias float32 [V] or None."""
-    import torch
-    (B, H), V = x.shape, int(codes.shape[0])
-    if codes.dim() != 2 or not codes.is_cuda or codes.dtype != torch.uint8 or (codes.shape[1] > 1 and codes.stride(1) != 1):
-        raise TypeError("codes must be a device matrix of contiguous rows in torch.uint8")
+    f32, bf16, u8, _ = _types()
+    rows, words, out = x.shape, codes.shape, y.shape
+    if len(rows) != 2 or len(words) != 2 or codes.dtype is not u8 or not codes.is_cuda:
+        raise TypeError("codes must be a device matrix in torch.uint8, x a matrix")
     if group not in (32, 64, 128):
         raise ValueError("group must be 32, 64 or 128")
-    shape = (-(-H // group), V)
-    if y.shape != (B, V) or codes.shape[1] < -(-H // 2) or scales.shape != shape or (zeros is not None and zeros.shape != shape) or \
-            (bias is not None and bias.shape != (V,)):
+    (B, H), (V, row) = rows, words
+    code_ld, one = codes.stride()
+    if out != (B, V) or 2 * row < H or (one != 1 and row > 1):
         raise TypeError("shape mismatch")
-    if scales.dtype not in (torch.float32, torch.bfloat16):
+    groups = (-(-H // group), V)
+    scale_type = scales.dtype
+    if scale_type is not f32 and scale_type is not bf16:
         raise TypeError("scales must be float32 or bfloat16")
-    (px, ldx, tx), (py, ldy, ty) = _rows(x, "x"), _rows(y, "y")
-    code_ld = int(codes.stride(0)) if V > 1 else max(int(codes.stride(0)), int(codes.shape[1]))
-    _check(lib().rnnlm_q4_matvec(int(B), V, int(H), int(group), codes.data_ptr() or None, code_ld,
-                                 RNNLM_F32 if scales.dtype == torch.float32 else RNNLM_BF16, _dev(scales, scales.dtype, "scales"),
-                                 _dev(zeros, torch.uint8, "zeros"), _dev(bias, torch.float32, "bias"), tx, px, ldx, ty, py, ldy,
-                                 _stream(stream)), "rnnlm_q4_matvec")
+    px, ldx, tx = _rows(x, rows, "x")
+    py, ldy, ty = _rows(y, out, "y")
+    status = _lib.rnnlm_q4_matvec(B, V, H, group, codes.data_ptr() or None, code_ld if V > 1 else max(code_ld, row),
+                                  RNNLM_F32 if scale_type is f32 else RNNLM_BF16, _same(scales, scale_type, groups, "scales"),
+                                  None if zeros is None else _same(zeros, u8, groups, "zeros"),
+                                  None if bias is None else _same(bias, f32, (V,), "bias"), tx, px, ldx, ty, py, ldy, _stream(stream))
+    if status:
+        _check(status, "rnnlm_q4_matvec")
 
 
 def rnnlm_q4_quantize(w: np.ndarray, group: int, zeros: bool = False):
@@ -582,34 +621,39 @@ def rnnlm_sample(logits, u, word, logprob, workspace, temperature=None, top_k=No
     """A word from each row of logits [N,V] (float32 or bfloat16) by the uniform numbers u [N]; temperature, top_p, min_p float32
     [N] or None, top_k int32 [N] or None; word int32 [N] out, logprob float32 [N] out or None; workspace uint8 device tensor of
     rnnlm_sample_workspace_bytes(N, V)."""
-    import torch
-    N, V = logits.shape
-    if any(t is not None and t.shape != (N,) for t in (u, word, logprob, temperature, top_k, top_p, min_p)):
-        raise TypeError("shape mismatch")
-    p, ld, code = _rows(logits, "logits")
-    _check(lib().rnnlm_sample(int(N), int(V), code, p, ld, _dev(temperature, torch.float32, "temperature"),
-                              _dev(top_k, torch.int32, "top_k"), _dev(top_p, torch.float32, "top_p"),
-                              _dev(min_p, torch.float32, "min_p"), _dev(u, torch.float32, "u"), _dev(word, torch.int32, "word"),
-                              _dev(logprob, torch.float32, "logprob"), _dev(workspace, torch.uint8, "workspace"),
-                              0 if workspace is None else workspace.numel(), _stream(stream)), "rnnlm_sample")
+    f32, _, _, i32 = _types()
+    shape = logits.shape
+    p, ld, code = _rows(logits, shape, "logits")
+    N, V = shape
+    n = (N,)
+    ws, ws_bytes = _space(workspace)
+    status = _lib.rnnlm_sample(N, V, code, p, ld, _same(temperature, f32, n, "temperature"), _same(top_k, i32, n, "top_k"),
+                               _same(top_p, f32, n, "top_p"), _same(min_p, f32, n, "min_p"), _same(u, f32, n, "u"),
+                               _same(word, i32, n, "word"), _same(logprob, f32, n, "logprob"), ws, ws_bytes, _stream(stream))
+    if status:
+        _check(status, "rnnlm_sample")
 
 
 def rnnlm_distill_workspace_bytes(N: int, V: int) -> int:
     return int(lib().rnnlm_distill_workspace_bytes(int(N), int(V)))
 
 
-def _distill_args(logits, teacher_word, teacher_logit, labels, row_weight, stats, grad):
-    import torch
-    N, V = logits.shape
-    K = int(teacher_word.shape[1]) if teacher_word.dim() == 2 else 0
-    if teacher_word.shape != (N, K) or teacher_logit.shape != (N, K) or stats.shape != (N, 4) or \
-            (labels is not None and labels.shape != (N,)) or (row_weight is not None and row_weight.shape != (N,)) or \
-            (grad is not None and grad.shape != (N, V)):
+def _distill_args(logits, teacher_word, teacher_logit, labels):
+    f32, _, _, i32 = _types()
+    shape = logits.shape
+    p, ld, code = _rows(logits, shape, "logits")
+    N, V = shape
+    listed = teacher_word.shape
+    if len(listed) != 2 or listed[0] != N:
         raise TypeError("shape mismatch")
-    p, ld, code = _rows(logits, "logits")
-    pg, ldg, _ = (None, 0, 0) if grad is None else _rows(grad, "grad", logits.dtype)
-    return (int(N), int(V), K, code, p, ld, _dev(teacher_word, torch.int32, "teacher_word"),
-            _dev(teacher_logit, torch.float32, "teacher_logit"), _dev(labels, torch.int32, "labels")), (pg, ldg)
+    return N, V, listed[1], code, p, ld, _same(teacher_word, i32, listed, "teacher_word"), \
+        _same(teacher_logit, f32, listed, "teacher_logit"), _same(labels, i32, (N,), "labels")
+
+
+def _grad_rows(grad, logits):
+    if grad.dtype is not logits.dtype or grad.shape != logits.shape:
+        raise TypeError("grad must have the shape and type of the logits")
+    return _rows(grad, grad.shape, "grad")[:2]
 
 
 def rnnlm_distill(logits, teacher_word, teacher_logit, loss, stats, workspace, temperature: float = 1.0, labels=None,
@@ -617,20 +661,23 @@ def rnnlm_distill(logits, teacher_word, teacher_logit, loss, stats, workspace, t
     """Loss [N] of logits [N,V] (float32 or bfloat16) against teacher_word int32 / teacher_logit float32 [N,K] and labels int32 [N] or
     None; stats float32 [N,4] out; grad [N,V] of the logits' type out, or None; row_weight float32 [N] or None: what the loss of each
     row weighs in the gradient; workspace uint8 device tensor of rnnlm_distill_workspace_bytes(N, V)."""
-    import torch
-    a, (pg, ldg) = _distill_args(logits, teacher_word, teacher_logit, labels, row_weight, stats, grad)
-    if loss.shape != (a[0],):
-        raise TypeError("shape mismatch")
-    _check(lib().rnnlm_distill(*a, float(temperature), float(label_weight), _dev(row_weight, torch.float32, "row_weight"),
-                               _dev(loss, torch.float32, "loss"), _dev(stats, torch.float32, "stats"), pg, ldg,
-                               _dev(workspace, torch.uint8, "workspace"), 0 if workspace is None else workspace.numel(),
-                               _stream(stream)), "rnnlm_distill")
+    a = _distill_args(logits, teacher_word, teacher_logit, labels)
+    f32, N = _torch_types[0], a[0]
+    pg, ldg = (None, 0) if grad is None else _grad_rows(grad, logits)
+    ws, ws_bytes = _space(workspace)
+    status = _lib.rnnlm_distill(*a, temperature, label_weight, _same(row_weight, f32, (N,), "row_weight"), _same(loss, f32, (N,), "loss"),
+                                _same(stats, f32, (N, 4), "stats"), pg, ldg, ws, ws_bytes, _stream(stream))
+    if status:
+        _check(status, "rnnlm_distill")
 
 
 def rnnlm_distill_backward(logits, teacher_word, teacher_logit, stats, grad, temperature: float = 1.0, labels=None,
                            label_weight: float = 0.0, row_weight=None, stream=None):
     """The gradient of rnnlm_distill's loss from the stats it left."""
-    import torch
-    a, (pg, ldg) = _distill_args(logits, teacher_word, teacher_logit, labels, row_weight, stats, grad)
-    _check(lib().rnnlm_distill_backward(*a, float(temperature), float(label_weight), _dev(row_weight, torch.float32, "row_weight"),
-                                        _dev(stats, torch.float32, "stats"), pg, ldg, _stream(stream)), "rnnlm_distill_backward")
+    a = _distill_args(logits, teacher_word, teacher_logit, labels)
+    f32, N = _torch_types[0], a[0]
+    pg, ldg = _grad_rows(grad, logits)
+    status = _lib.rnnlm_distill_backward(*a, temperature, label_weight, _same(row_weight, f32, (N,), "row_weight"),
+                                         _same(stats, f32, (N, 4), "stats"), pg, ldg, _stream(stream))
+    if status:
+        _check(status, "rnnlm_distill_backward")
