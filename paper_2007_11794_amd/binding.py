@@ -528,15 +528,16 @@ def rnnlm_hs_time_query(model: RnnlmModel, query_word, h_out, logprob, repeats: 
     return ms.value
 
 
-_torch_types = None
+_torch_types = _raw_stream = _device = None
 
 
 def _types():
-    """(float32, bfloat16, uint8, int32) of torch, looked up once."""
-    global _torch_types
+    """(float32, bfloat16, uint8, int32) of torch, looked up once, with the two functions of _stream_of."""
+    global _torch_types, _raw_stream, _device
     if _torch_types is None:
         import torch
         lib()
+        _raw_stream, _device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
         _torch_types = (torch.float32, torch.bfloat16, torch.uint8, torch.int32)
     return _torch_types
 
@@ -563,6 +564,11 @@ def _same(t, dtype, shape, name):
     if t.dtype is not dtype or not t.is_cuda or not t.is_contiguous():
         raise TypeError("%s must be a contiguous device tensor of dtype %s" % (name, dtype))
     return t.data_ptr() or None
+
+
+def _stream_of(stream) -> Optional[int]:
+    """_stream() behind the check of a device tensor, which only an initialised device gives."""
+    return _stream(stream) if stream is not None else _raw_stream(_device()) or None
 
 
 def _space(workspace):
@@ -594,7 +600,7 @@ def rnnlm_q4_matvec(codes, scales, group: int, x, y, zeros=None, bias=None, stre
     status = _lib.rnnlm_q4_matvec(B, V, H, group, codes.data_ptr() or None, code_ld if V > 1 else max(code_ld, row),
                                   RNNLM_F32 if scale_type is f32 else RNNLM_BF16, _same(scales, scale_type, groups, "scales"),
                                   None if zeros is None else _same(zeros, u8, groups, "zeros"),
-                                  None if bias is None else _same(bias, f32, (V,), "bias"), tx, px, ldx, ty, py, ldy, _stream(stream))
+                                  None if bias is None else _same(bias, f32, (V,), "bias"), tx, px, ldx, ty, py, ldy, _stream_of(stream))
     if status:
         _check(status, "rnnlm_q4_matvec")
 
@@ -629,7 +635,7 @@ def rnnlm_sample(logits, u, word, logprob, workspace, temperature=None, top_k=No
     ws, ws_bytes = _space(workspace)
     status = _lib.rnnlm_sample(N, V, code, p, ld, _same(temperature, f32, n, "temperature"), _same(top_k, i32, n, "top_k"),
                                _same(top_p, f32, n, "top_p"), _same(min_p, f32, n, "min_p"), _same(u, f32, n, "u"),
-                               _same(word, i32, n, "word"), _same(logprob, f32, n, "logprob"), ws, ws_bytes, _stream(stream))
+                               _same(word, i32, n, "word"), _same(logprob, f32, n, "logprob"), ws, ws_bytes, _stream_of(stream))
     if status:
         _check(status, "rnnlm_sample")
 
@@ -666,7 +672,7 @@ def rnnlm_distill(logits, teacher_word, teacher_logit, loss, stats, workspace, t
     pg, ldg = (None, 0) if grad is None else _grad_rows(grad, logits)
     ws, ws_bytes = _space(workspace)
     status = _lib.rnnlm_distill(*a, temperature, label_weight, _same(row_weight, f32, (N,), "row_weight"), _same(loss, f32, (N,), "loss"),
-                                _same(stats, f32, (N, 4), "stats"), pg, ldg, ws, ws_bytes, _stream(stream))
+                                _same(stats, f32, (N, 4), "stats"), pg, ldg, ws, ws_bytes, _stream_of(stream))
     if status:
         _check(status, "rnnlm_distill")
 
@@ -678,6 +684,6 @@ def rnnlm_distill_backward(logits, teacher_word, teacher_logit, stats, grad, tem
     f32, N = _torch_types[0], a[0]
     pg, ldg = _grad_rows(grad, logits)
     status = _lib.rnnlm_distill_backward(*a, temperature, label_weight, _same(row_weight, f32, (N,), "row_weight"),
-                                         _same(stats, f32, (N, 4), "stats"), pg, ldg, _stream(stream))
+                                         _same(stats, f32, (N, 4), "stats"), pg, ldg, _stream_of(stream))
     if status:
         _check(status, "rnnlm_distill_backward")
