@@ -280,3 +280,20 @@ def test_no_rows():
     e, i = torch.empty, torch.int32
     rn.rnnlm_distill(e((0, 9), device=DEV), e((0, 3), dtype=i, device=DEV), e((0, 3), device=DEV), e(0, device=DEV), e((0, 4), device=DEV), None)
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("N,V,K", [(3, 5000, 4096), (2, 70001, 4096), (130, 9000, 2000), (2, 100000, 1500)])
+def test_long_lists(N, V, K):
+    d = case(N, V, K)
+    d["words"][0, 100:200] = d["words"][0, :100].clone()           # and words that repeat in one of them
+    loss, stats, grad = run(d, 2.0, 0.25)
+    check(d, 2.0, 0.25, loss, grad, rows=range(min(N, 4)))
+    check(d, 2.0, 0.25, loss, backward(d, 2.0, 0.25, stats), rows=range(min(N, 4)))
+
+
+def test_a_row_that_weighs_nothing():
+    d = case(3, 3000, 20)
+    d["g"][1] = 0.0
+    loss, stats, grad = run(d, 2.0, 0.3)
+    check(d, 2.0, 0.3, loss, grad)
+    assert bool((grad[1] == 0).all()) and bool((backward(d, 2.0, 0.3, stats)[1] == 0).all())

@@ -224,3 +224,35 @@ def test_another_stream_and_a_graph(N, V):
         torch.cuda.synchronize()
         assert np.array_equal(word.cpu().numpy(), want[i][0]) and np.array_equal(lp.cpu().numpy(), want[i][1])
         assert np.array_equal(draw(zs[2], u, T, k, p, m)[0], want[2][0])
+
+
+def test_a_row_of_seventy_million_words():
+    """More segments than the last launch has places in LDS for their sums: a few thousand words among seventy million."""
+    V, some = 70000001, 5000
+    rng = np.random.default_rng(1)
+    at = np.sort(rng.choice(V, some, replace=False))
+    at[-1] = V - 1
+    z = torch.full((3, V), -INF, device=DEV, dtype=torch.bfloat16)
+    value = torch.from_numpy(rng.standard_normal((3, some)).astype(np.float32)).to(torch.bfloat16)
+    z[:, torch.from_numpy(at).to(DEV)] = value.to(DEV)
+    for a in (dict(), dict(k=[0, 40, 3000]), dict(p=[0.3, 0.9, 0.999]), dict(k=[4000, 70000000, 100], p=[0.5, 0.7, 1.0], m=[0.0, 0.05, 0.3]), dict(T=[0.0, 0.5, 3.0])):
+        u = rng.random(3).astype(np.float32) * np.float32(0.99999)
+        word, _ = draw(z, u, **a)
+        for n in range(3):
+            want = sample_row(value[n].double().numpy(), float(u[n]), *(np.float64(np.float32(a[x][n])) if x in a else o for x, o in (("T", 1.0),)),
+                              int(a["k"][n]) if "k" in a else 0, *(np.float64(np.float32(a[x][n])) if x in a else o for x, o in (("p", 1.0), ("m", 0.0))))
+            assert word[n] == at[want[0]], (a, n)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_long_rows_with_many_words_kept(dtype):
+    """Limits that leave more words than a list holds, with and without a limit on their weight behind it."""
+    V = 150001
+    z = logits(6, V, 21, dtype, spread=0.3)
+    u = np.linspace(0.05, 0.95, 6).astype(np.float32)
+    check(z, u, k=[20000, 60000, 149000, 5000, 30000, 100000])
+    check(z, u, k=[20000, 60000, 149000, 5000, 30000, 100000], p=[0.9, 0.5, 0.99, 0.3, 0.7, 0.999])
+    check(z, u, p=[0.9, 0.5, 0.99, 0.3, 0.7, 0.9999], m=[0.0, 1e-4, 0.0, 0.01, 0.0, 1e-6])
+    flat = torch.zeros((6, V), device=DEV, dtype=dtype)
+    flat[:, 1::2] = 1.0
+    check(flat, u, k=[20000, 60000, 149000, 5000, 30000, 100000], p=[0.9, 1.0, 0.5, 1.0, 0.7, 1.0])

@@ -141,3 +141,15 @@ def test_plain_gradient_against_differences(T, a):
         down[i] -= e
         # the second difference's error is e^2 / 6 times a third derivative below T^-1 + 1 in magnitude; rounding is 2^-52 * 10 / e
         assert abs((distill_row(up, words, t, 4, T, a)[0] - distill_row(down, words, t, 4, T, a)[0]) / (2 * e) - grad[i]) < 1e-9
+
+
+def test_more_teacher_entries_than_a_list_holds():
+    assert distill(K=4097) == ERANGE and distill(N=0, K=4096) == 0
+
+
+def test_interleaved_rows_are_no_overlap():
+    """Rows of the gradient in the gaps of the logits' rows: nothing is shared, and nothing but the workspace is refused."""
+    assert distill(z=at(0), ld=16, grad=at(32), gld=16, ws=None) == EWORKSPACE
+    assert distill(z=at(0), ld=16, grad=at(28), gld=16, ws=at(4096)) == EINVAL
+    assert distill(z=at(0), ld=16, grad=at(68), gld=16, ws=at(4096)) == EINVAL
+    assert distill(z=at(0), ld=16, grad=at(32), gld=17, ws=at(4096)) == EINVAL
