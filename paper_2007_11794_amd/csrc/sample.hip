@@ -46,20 +46,19 @@ __device__ __forceinline__ double fma_with(double a, double b, double c) {
 }
 
 // 2^y for y <= 0 as a whole number of 2^-bits, to nearest (bits <= 50; anything below -200 is nothing).  2^f on [-1/2, 1/2] is 1 + f times a polynomial fitted for the
-// least relative error, 1.5e-14.  Sums and products alone, at full rate: the nearest whole number n comes of adding 1.5 * 2^52 and taking it
+// least relative error, 8.1e-13 (which moves a border between two words by that share of the sum).  Sums and products alone, at full rate: the nearest whole number n comes of adding 1.5 * 2^52 and taking it
 // off, its power of two goes into the exponent, and the result is rounded by adding 2^52, below which the last bit counts 1 (with the
 // instructions for rounding, conversion and scaling, a quarter of that rate each, 65536 weights took a workgroup 17.7 us for this).
 __device__ __forceinline__ u64 fixed_exp2(double y, int bits) {
     y = fmax(y, -200.0);
     const double t = y + 0x1.8p52, f = y - (t - 0x1.8p52);
-    double q = fma_with(0x1.b3de2c7e1dde3p-24, f, 0x1.63e69680bde3cp-20);
-    q = fma_with(q, f, 0x1.ffce2fc63d69ep-17);
-    q = fma_with(q, f, 0x1.430897f31267cp-13);
-    q = fma_with(q, f, 0x1.5d87fd9386691p-10);
-    q = fma_with(q, f, 0x1.3b2ab72412393p-7);
-    q = fma_with(q, f, 0x1.c6b08d70c8822p-5);
-    q = fma_with(q, f, 0x1.ebfbdff81be04p-3);
-    q = fma_with(q, f, 0x1.62e42fefa37d1p-1);
+    double q = fma_with(0x1.61c4f05b35904p-20, f, 0x1.00d8538df1462p-16);
+    q = fma_with(q, f, 0x1.430aa8842f4a4p-13);
+    q = fma_with(q, f, 0x1.5d874d067423fp-10);
+    q = fma_with(q, f, 0x1.3b2ab5ed6e014p-7);
+    q = fma_with(q, f, 0x1.c6b08dced3e72p-5);
+    q = fma_with(q, f, 0x1.ebfbdff8edeaap-3);
+    q = fma_with(q, f, 0x1.62e42fef89d19p-1);
     q = fma(q, f, 1.0);
     const uint32_t n = (uint32_t)__double_as_longlong(t) + (uint32_t)bits;
     const u64 x = (u64)__double_as_longlong(q) + ((u64)(n << 20) << 32);
@@ -659,29 +658,39 @@ __global__ __launch_bounds__(THREADS, 4) void sample_row_kernel(SampleArgs a, in
 
 // ---- rows in segments
 
-constexpr int kSegThreads = 256, kSegVectors = 16, kLongBins = 4096, kPickThreads = 1024;
-template <typename Z> constexpr int segment_words() { return kSegThreads * kSegVectors * Row<Z>::E; }
+constexpr int kSegThreads = 256, kSegWaves = kSegThreads / 64, kSegVectors = 16, kLongHeld = 12288, kLongBins = 4096, kPickThreads = 1024;
+template <typename Z> __host__ __device__ constexpr int segment_words() { return kSegThreads * kSegVectors * Row<Z>::E; }
+// Words of a wave's part of the segment that word `from` begins, as Words lays them out.
+template <typename Z> __device__ __forceinline__ int part_words(int V, int from) {
+    const int len = min(V - from, segment_words<Z>());
+    return ((len + Row<Z>::E - 1) / Row<Z>::E + kSegThreads - 1) / kSegThreads * 64 * Row<Z>::E;
+}
 
 // Words that can be listed of a row in memory.  In bfloat16 a bin is one logit, and some hundredth of the words may have it.
 __host__ __device__ constexpr int long_list(int V) { return V / 16 > 8192 ? V / 16 : 8192; }
 
 // Of one row in the workspace, behind its histogram of kLongBins weights (or counts): the deciding bin and what is wanted of it, the words listed,
-// how many there are, and of every segment its maximum and the weight of its words that are kept for certain.
+// how many there are, of every segment its maximum, and of every wave's quarter of one the weight of its words that are kept for certain.
 struct LongRow {
     u64 *hist, *list, *sums;
     u64 *want;
     int *bin, *listed;
     float *tops;
-    static __host__ __device__ size_t bytes(int V, int segments) { return (size_t)(kLongBins + long_list(V) + segments) * 8 + 16 + ((size_t)segments * 4 + 15) / 16 * 16; }
+    static __host__ __device__ size_t bytes(int V, int segments) { return (size_t)(kLongBins + long_list(V) + segments * kSegWaves) * 8 + 16 + ((size_t)segments * 4 + 15) / 16 * 16; }
     __device__ LongRow(void *ws, int n, int V, int segments) {
         char *p = static_cast<char *>(ws) + n * bytes(V, segments);
         hist = reinterpret_cast<u64 *>(p);
         list = hist + kLongBins;
         sums = list + long_list(V);
-        want = sums + segments;
+        want = sums + segments * kSegWaves;
         bin = reinterpret_cast<int *>(want + 1);
         listed = bin + 1;
         tops = reinterpret_cast<float *>(listed + 1);
+    }
+    // Segment s: the sum over this wave of `sum`.
+    __device__ __forceinline__ void put_sum(int s, u64 sum) const {
+        sum = wave_scan64(sum);
+        if ((threadIdx.x & 63) == 63) sums[s * kSegWaves + (threadIdx.x >> 6)] = sum;
     }
     // The row's maximum; NaN where there is one.
     template <int THREADS, typename S>
@@ -730,7 +739,7 @@ __global__ __launch_bounds__(kSegThreads) void sample_weigh_kernel(SampleArgs a,
     Search<kSegThreads, kLongBins, 1> search(sh, scale, 0, a.V);
     auto over = [&](auto f) { words.each(scale.alike, from, f); };
     if (!l.few(a.V) && !l.part()) {
-        u64 sum = 0, total;
+        u64 sum = 0;
         over([&](auto some) {
 #pragma unroll
             for (int j = 0; j < some.M; ++j) {
@@ -738,8 +747,7 @@ __global__ __launch_bounds__(kSegThreads) void sample_weigh_kernel(SampleArgs a,
                 sum += some.z[j] > -INFINITY ? w : 0;
             }
         });
-        block_scan64<kSegThreads>(sum, sh, total);
-        if (threadIdx.x == 0) r.sums[s] = total;
+        r.put_sum(s, sum);
         return;
     }
     const bool counts = l.few(a.V);
@@ -787,14 +795,15 @@ __global__ __launch_bounds__(kSegThreads) void sample_gather_kernel(SampleArgs a
             sum += some.z[j] > -INFINITY && scale.bin_of(some.z[j]) < bin ? w : 0;
         }
     });
-    block_scan64<kSegThreads>(sum, sh, total);
-    if (tid == 0) r.sums[s] = total;
+    r.put_sum(s, sum);
 }
 
 template <typename Z>
 __global__ __launch_bounds__(kPickThreads, 4) void sample_pick_kernel(SampleArgs a, int segments, int bits) {
     constexpr int BINS = kLongBins;
-    __shared__ Shared<BINS, 1> sh;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    Shared<BINS, 1> &sh = *reinterpret_cast<Shared<BINS, 1> *>(lds);
+    u64 *const held = reinterpret_cast<u64 *>(lds + sizeof(Shared<BINS, 1>));
     const int tid = threadIdx.x, n = blockIdx.x, V = a.V;
     const Limits l(a, n);
     const LongRow r(a.ws, n, a.V, segments);
@@ -840,13 +849,20 @@ __global__ __launch_bounds__(kPickThreads, 4) void sample_pick_kernel(SampleArgs
     };
     const bool all = lists_all(l, V), of_bin = lists_bin(l, V);
     const int listed = all || of_bin ? *r.listed : 0;
+    // (several passes go over the list: it stays in LDS where it fits)
+    const u64 *list = r.list;
+    if (listed <= kLongHeld) {
+        for (int i = tid; i < listed; i += kPickThreads) held[i] = r.list[i];
+        list = held;
+        __syncthreads();
+    }
     auto over_list = [&](auto f) {
         for (int i0 = 0; i0 < listed; i0 += 8 * kPickThreads) {
             u64 w[8];
 #pragma unroll
             for (int q = 0; q < 8; ++q) {
                 const int i = i0 + q * kPickThreads + tid;
-                w[q] = i < listed ? r.list[i] : 0;
+                w[q] = i < listed ? list[i] : 0;
             }
 #pragma unroll 1
             for (int q = 0; q < 8 && i0 + q * kPickThreads < listed; ++q) {
@@ -864,7 +880,8 @@ __global__ __launch_bounds__(kPickThreads, 4) void sample_pick_kernel(SampleArgs
     } else if (all) {
         total = search.all_steps(l, V, over_list);
     } else {
-        const bool in_lds = segments <= BINS;                 // what the bin's words add to the segments' sums
+        const int parts = segments * kSegWaves;
+        const bool in_lds = parts <= BINS;                    // what the bin's words add to the parts' sums
         for (int i = tid; i < BINS; i += kPickThreads) sh.weight[i] = 0;
         if (of_bin && listed) {
             const int bin = *r.bin;
@@ -876,29 +893,30 @@ __global__ __launch_bounds__(kPickThreads, 4) void sample_pick_kernel(SampleArgs
             over_list([&](auto some) {
                 if (!search.kept(some.z[0], some.id[0]) || scale.bin_of(some.z[0]) != bin) return;
                 const u64 w = search.weigh(kDraw, some.z[0]);
-                const int s = some.id[0] / segment_words<Z>();
+                const int seg = some.id[0] / segment_words<Z>(), from = seg * segment_words<Z>(), s = seg * kSegWaves + ((int)some.id[0] - from) / part_words<Z>(V, from);
                 if (in_lds) atomicAdd(&sh.weight[s], w);
                 else __hip_atomic_fetch_add(&r.sums[s], w, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
             });
             seen_by_all();
         }
         __syncthreads();
-        auto sum_of = [&](int s) { return s < segments ? __hip_atomic_load(&r.sums[s], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + (in_lds ? sh.weight[s] : 0) : 0ull; };
-        u64 sum = 0, part;
-        for (int s = tid; s < segments; s += kPickThreads) sum += sum_of(s);
+        auto sum_of = [&](int s) { return s < parts ? __hip_atomic_load(&r.sums[s], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + (in_lds ? sh.weight[s] : 0) : 0ull; };
+        u64 sum = 0, in_turn;
+        for (int s = tid; s < parts; s += kPickThreads) sum += sum_of(s);
         block_scan64<kPickThreads>(sum, sh, total);
         const u64 target = l.target(total);
         if (tid == 0) sh.bin = 0;
         u64 before = 0;
-        for (int s0 = 0; s0 < segments; s0 += kPickThreads) {         // the segment that has it, and what lies in front of it
-            const u64 mine = sum_of(s0 + tid), upto = before + block_scan64<kPickThreads>(mine, sh, part);
+        for (int s0 = 0; s0 < parts; s0 += kPickThreads) {            // the part that has it, and what lies in front of it
+            const u64 mine = sum_of(s0 + tid), upto = before + block_scan64<kPickThreads>(mine, sh, in_turn);
             if (upto - mine <= target && target < upto) { sh.bin = s0 + tid; sh.want = target - (upto - mine) + 1; }
-            before += part;
+            before += in_turn;
         }
         __syncthreads();
-        const int s = __builtin_amdgcn_readfirstlane(sh.bin), from = s * segment_words<Z>(), to = min(V, from + segment_words<Z>());
+        const int s = __builtin_amdgcn_readfirstlane(sh.bin), segment = s / kSegWaves * segment_words<Z>(), part_of = part_words<Z>(V, segment);
+        const int from = segment + s % kSegWaves * part_of, to = min(V, from + part_of);
         const u64 wanted = uniform(sh.want);
-        const Words<Z, kPickThreads, kSegThreads * kSegVectors / kPickThreads> words(row + from, to - from);
+        const Words<Z, kPickThreads, 4> words(row + from, to - from);
         draw_from_registers<kPickThreads>(words, sh, scale, l, search.border, from, [&](u64) { return wanted - 1; });
     }
     answer(a, n, sh.word, log_share(sh.found_w, total));
@@ -926,10 +944,14 @@ hipError_t launch(const SampleArgs &a, int bits, hipStream_t stream) {
     const int segments = segments_of<Z>(a.V);
     if ((long long)a.N * segments > 0x7FFFFFFF) return hipErrorInvalidValue;
     const int groups = a.N * segments;
+    static LdsLimit limit;
+    constexpr size_t pick_bytes = sizeof(Shared<kLongBins, 1>) + (size_t)kLongHeld * 8;
+    const hipError_t e = limit.ensure(reinterpret_cast<const void *>(sample_pick_kernel<Z>), pick_bytes);
+    if (e != hipSuccess) return e;
     sample_tops_kernel<Z><<<groups, kSegThreads, 0, stream>>>(a, segments);
     sample_weigh_kernel<Z><<<groups, kSegThreads, 0, stream>>>(a, segments, bits);
     sample_gather_kernel<Z><<<groups, kSegThreads, 0, stream>>>(a, segments, bits);
-    sample_pick_kernel<Z><<<a.N, kPickThreads, 0, stream>>>(a, segments, bits);
+    sample_pick_kernel<Z><<<a.N, kPickThreads, pick_bytes, stream>>>(a, segments, bits);
     return hipGetLastError();
 }
 
