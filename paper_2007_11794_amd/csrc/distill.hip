@@ -568,9 +568,11 @@ Cut cut_row(int V, int E, int segments) {
     return Cut{(vectors + per - 1) / per, per * E};
 }
 
-// Rows too few to fill the chip by one workgroup each, and long enough to cut.
-int segments_of(int N, int V) {
-    if (N >= 128 || V < 8192) return 1;
+// Rows too few to fill the chip by one workgroup each, and so long that one compute unit's way to memory (some 80 GB/s) takes longer than a
+// second launch.  Steps, us, a workgroup a row / segments: fp32, V = 65536: 1 row 14.7 / 13.2, 16 rows 15.3 / 13.1, 64 rows 18.0 / 18.5, 100 rows
+// 19.1 / 25.3; V = 200000: 100 rows 55.7 / 75.4; V = 20000: 8 rows 10.1 / 13.1, the loss alone 9.1 / 12.2.
+int segments_of(int N, int V, bool bf16) {
+    if (N > 48 || (long long)V * (bf16 ? 2 : 4) < 192 * 1024) return 1;
     int s = 2 * kChipGroups / N;
     if (s > V / 4096) s = V / 4096;
     return s < 2 ? 1 : s > kMaxSegments ? kMaxSegments : s;
@@ -579,7 +581,7 @@ int segments_of(int N, int V) {
 template <typename Z>
 hipError_t forward(const DistillArgs &a, hipStream_t stream) {
     constexpr int E = Row<Z>::E;
-    const int s = segments_of(a.N, a.V);
+    const int s = segments_of(a.N, a.V, a.bf16);
     if (s > 1) {
         static LdsLimit limit;
         const size_t bytes = list_bytes(a.K);
@@ -608,7 +610,7 @@ hipError_t backward(const DistillArgs &a, hipStream_t stream) {
 }  // namespace
 
 size_t distill_workspace_bytes(int N, int V) {
-    const int s = segments_of(N, V);
+    const int s = segments_of(N, V, false);                 // (bfloat16 has no more)
     return s > 1 ? (size_t)N * s * sizeof(Part) : 16;
 }
 

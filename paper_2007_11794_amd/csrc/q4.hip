@@ -5,7 +5,7 @@
 // group: no weight is ever rounded.  An fp32 x is two fp16 terms relative to its row's largest magnitude (two products instead of one), a
 // bf16 x is one.
 //
-// One wave takes NT tiles of 16 words by 16 * MT rows.  Its B operand (16x16x32: lane = word, 8 units) comes straight from memory: a
+// One wave takes 16 words by 16 * MT rows.  Its B operand (16x16x32: lane = word, 8 units) comes straight from memory: a
 // lane loads 16 bytes, 32 consecutive codes of its word, the four lanes of a word 64 consecutive bytes; a transpose of 4 x 4 dwords over
 // those four lanes (four register swaps) turns "32 units of one group per lane" into "the same group in all four lanes", so that a matrix
 // instruction never mixes two groups, whatever their size.  The A operand, the rows, lies in LDS in operand order, staged once per workgroup.
@@ -20,13 +20,14 @@ constexpr int kThreads = 512, kWaves = kThreads / 64;
 constexpr int kStep = 128;                                   // units of a step: 16 bytes of codes a lane
 constexpr size_t kLdsRows = 144 * 1024;                      // most LDS for the rows' operands
 
+// Waves of a SIMD: as many as keep their requests in registers.  V = 1000000, H = 256, groups of 128, 1 row: 4 waves 42.8 us, 6 waves 37.9; groups
+// of 32, H = 100, 8 rows: 33.9 / 38.1.
+constexpr int waves_of(int MT, int G, bool zero) { return MT == 1 && (G == 128 || (G == 64 && !zero)) ? 6 : 4; }
+
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef u32x4 u32x4_any __attribute__((aligned(1)));         // rows of codes may start anywhere
 
 typedef f32x4 f32x4_any __attribute__((aligned(4)));
-typedef uint64_t u64_any __attribute__((aligned(2)));
-typedef uint32_t u32_any __attribute__((aligned(1)));
-typedef uint16_t u16_any __attribute__((aligned(1)));
 
 // Elements k .. k + 7 of a row of H, 0 behind it.
 __device__ __forceinline__ void eight_of_row(const void *x, long long at, int k, int H, bool bf16, float (&out)[8]) {
@@ -48,13 +49,13 @@ __device__ __forceinline__ void eight_of_row(const void *x, long long at, int k,
     }
 }
 
-// What a wave needs of one step of NT tiles of 16 words, as it comes from memory.
-template <int NT, int GROUPS, bool ZERO>
+// What a wave needs of one step of a tile of 16 words, as it comes from memory.
+template <int GROUPS, bool ZERO>
 struct Codes {
-    u32x4 w[NT];
-    uint64_t scale[GROUPS];              // NT of them, of either type
+    u32x4 w;
+    uint32_t scale[GROUPS];              // of either type
     uint32_t zero[ZERO ? GROUPS : 1];
-    float bias[NT];                      // with the last step of a tile: a load behind the requests of later steps would have to wait for them
+    float bias;                          // with the last step of a tile: a load behind the requests of later steps would have to wait for them
 };
 
 // (w & mask) | exponents in one instruction (of two literals it takes none, and the compiler makes two)
@@ -94,8 +95,8 @@ __device__ __forceinline__ u32x4 without(u32x4 w, uint32_t n) {
     return u32x4{(uint32_t)x, (uint32_t)(x >> 32), (uint32_t)y, (uint32_t)(y >> 32)};
 }
 
-template <int TERMS, int MT, int NT, int G, bool ZERO>
-__global__ __launch_bounds__(kThreads, 4) void q4_kernel(Q4Args a, int chunk_steps, int rounds) {
+template <int TERMS, int MT, int G, bool ZERO>
+__global__ __launch_bounds__(kThreads, waves_of(MT, G, ZERO)) void q4_kernel(Q4Args a, int chunk_steps, int rounds) {
     constexpr int kRows = 16 * MT, kGroups = kStep / G;
     extern __shared__ __attribute__((aligned(1024))) char lds[];        // [units of a chunk / 32][MT][TERMS][64 lanes][8]
     __shared__ uint32_t row_top[kRows];                                 // the row's largest finite magnitude
@@ -103,61 +104,46 @@ __global__ __launch_bounds__(kThreads, 4) void q4_kernel(Q4Args a, int chunk_ste
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 15, g = lane >> 4;
     const int r0 = blockIdx.y * kRows, rows = a.B - r0 < kRows ? a.B - r0 : kRows;
     const int steps = (a.H + kStep - 1) / kStep, last_group = (a.H + G - 1) / G - 1, stride = gridDim.x * kWaves;
-    const int tiles = (a.V + 16 * NT - 1) / (16 * NT), scale_size = a.scale_bf16 ? 2 : 4;
+    const int tiles = (a.V + 15) / 16, scale_size = a.scale_bf16 ? 2 : 4;
     const uint8_t *const end = a.codes + (long long)(a.V - 1) * a.code_ld + ((a.H + 1) >> 1), *const last = end - 16;
 
     // Tiles from here on may have loads that pass the end of the codes: a lane's last one ends up to 63 bytes behind its row.
-    const int clear = (a.V - 64) / (16 * NT);
+    const int clear = (a.V - 64) / 16;
     // Requests run two steps ahead of the products, over the ends of tiles.
     int tile_r = blockIdx.x * kWaves + wave, step_r = 0;
-    const uint8_t *word_r[NT];
-    uint32_t v_r;                                                       // first word of a lane, in the array whatever the tile
+    const uint8_t *word_r;
+    uint32_t v_r;                                                       // a lane's word, in the array whatever the tile
     auto set_tile = [&]() {
-        const int v = tile_r * 16 * NT + NT * c, top = a.V - NT;        // (two words of a lane: V > 1)
-        v_r = (uint32_t)(v < top ? v : top);
-#pragma unroll
-        for (int n = 0; n < NT; ++n) word_r[n] = a.codes + (long long)(v + n < a.V ? v + n : a.V - 1) * a.code_ld + 16 * g;
+        const int v = tile_r * 16 + c;
+        v_r = (uint32_t)(v < a.V ? v : a.V - 1);
+        word_r = a.codes + (long long)v_r * a.code_ld + 16 * g;
     };
-    auto request = [&](Codes<NT, kGroups, ZERO> &q) {
+    auto request = [&](Codes<kGroups, ZERO> &q) {
         if (tile_r < tiles) {
-#pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                const uint8_t *p = word_r[n] + step_r * (kStep / 2);
-                if (tile_r < clear) {                                   // behind a row come the next one's bytes, times zeros
-                    q.w[n] = *reinterpret_cast<const u32x4_any *>(p);
-                } else if (last >= a.codes) {                           // the codes end: from further in front, see beyond()
-                    q.w[n] = *reinterpret_cast<const u32x4_any *>(p > last ? last : p);
-                } else {                                                // less than 16 bytes of codes in all
-                    uint32_t w[4] = {0, 0, 0, 0};
+            const uint8_t *p = word_r + step_r * (kStep / 2);
+            if (tile_r < clear) {                                       // behind a row come the next one's bytes, times zeros
+                q.w = *reinterpret_cast<const u32x4_any *>(p);
+            } else if (last >= a.codes) {                               // the codes end: from further in front, see below
+                q.w = *reinterpret_cast<const u32x4_any *>(p > last ? last : p);
+            } else {                                                    // less than 16 bytes of codes in all
+                uint32_t w[4] = {0, 0, 0, 0};
 #pragma unroll 1
-                    for (int i = 0; i < 16 && p + i < end; ++i) {
-                        const uint32_t byte = (uint32_t)p[i] << (8 * (i & 3));
+                for (int i = 0; i < 16 && p + i < end; ++i) {
+                    const uint32_t byte = (uint32_t)p[i] << (8 * (i & 3));
 #pragma unroll
-                        for (int d = 0; d < 4; ++d) w[d] |= i >> 2 == d ? byte : 0;
-                    }
-                    q.w[n] = u32x4{w[0], w[1], w[2], w[3]};
+                    for (int d = 0; d < 4; ++d) w[d] |= i >> 2 == d ? byte : 0;
                 }
+                q.w = u32x4{w[0], w[1], w[2], w[3]};
             }
 #pragma unroll
             for (int i = 0; i < kGroups; ++i) {
                 const int grp = step_r * kGroups + i < last_group ? step_r * kGroups + i : last_group;
                 const char *s = static_cast<const char *>(a.scale) + (long long)grp * a.V * scale_size;
-                if (a.scale_bf16) {
-                    if (NT == 2) q.scale[i] = *reinterpret_cast<const u32_any *>(s + v_r * 2u);
-                    else q.scale[i] = *reinterpret_cast<const uint16_t *>(s + v_r * 2u);
-                } else {
-                    if (NT == 2) q.scale[i] = *reinterpret_cast<const u64_any *>(s + v_r * 4u);
-                    else q.scale[i] = *reinterpret_cast<const uint32_t *>(s + v_r * 4u);
-                }
-                if (ZERO) {                                            
-                    const uint8_t *z = a.zero + (long long)grp * a.V;
-                    if (NT == 2) q.zero[i] = *reinterpret_cast<const u16_any *>(z + v_r);
-                    else q.zero[i] = z[v_r];
-                }
+                if (a.scale_bf16) q.scale[i] = *reinterpret_cast<const uint16_t *>(s + v_r * 2u);
+                else q.scale[i] = *reinterpret_cast<const uint32_t *>(s + v_r * 4u);
+                if (ZERO) q.zero[i] = (a.zero + (long long)grp * a.V)[v_r];
             }
-            if (step_r + 1 == steps)
-#pragma unroll
-                for (int n = 0; n < NT; ++n) q.bias[n] = a.bias ? a.bias[v_r + n] : 0.f;
+            if (step_r + 1 == steps) q.bias = a.bias ? a.bias[v_r] : 0.f;
         }
         if (++step_r == steps) {
             step_r = 0;
@@ -167,7 +153,7 @@ __global__ __launch_bounds__(kThreads, 4) void q4_kernel(Q4Args a, int chunk_ste
     };
 
     set_tile();
-    Codes<NT, kGroups, ZERO> q[3];
+    Codes<kGroups, ZERO> q[3];
     request(q[0]);
     request(q[1]);                                                      // on their way while the rows are staged
 
@@ -210,10 +196,10 @@ __global__ __launch_bounds__(kThreads, 4) void q4_kernel(Q4Args a, int chunk_ste
         }
     };
 
-    f32x4 acc[MT][NT];
+    f32x4 acc[MT];
     int tile = blockIdx.x * kWaves + wave, step = 0, left = rounds * steps, in_chunk = 0;
     bool staged = false;
-    auto body = [&](Codes<NT, kGroups, ZERO> &now, Codes<NT, kGroups, ZERO> &free) {
+    auto body = [&](Codes<kGroups, ZERO> &now, Codes<kGroups, ZERO> &free) {
         if (in_chunk == 0 && !(staged && chunk_steps >= steps)) {       // (the same in all waves)
             if (staged) __syncthreads();                                // the chunk before has been read
             const int n = steps - step < chunk_steps ? steps - step : chunk_steps;
@@ -225,93 +211,46 @@ __global__ __launch_bounds__(kThreads, 4) void q4_kernel(Q4Args a, int chunk_ste
         if (tile < tiles) {
             if (step == 0)
 #pragma unroll
-                for (int m = 0; m < MT; ++m)
-#pragma unroll
-                    for (int n = 0; n < NT; ++n) acc[m][n] = f32x4{0.f, 0.f, 0.f, 0.f};
-            const int v = tile * 16 * NT + NT * c;
-            bool edge = false;
-            u32x4 w[NT];
-#pragma unroll
-            for (int n = 0; n < NT; ++n) w[n] = now.w[n];
-            if (tile >= clear) {
-                // loads that began too early, and a lane's one word that was loaded as the second of two
-                edge = NT == 2 && v + 2 > a.V;
-#pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    const uint8_t *p = a.codes + (long long)(v + n < a.V ? v + n : a.V - 1) * a.code_ld + 16 * g + step * (kStep / 2);
-                    if (last >= a.codes && p > last) w[n] = without(w[n], p - last < 16 ? (uint32_t)(p - last) : 16u);
-                }
-                if (edge) {
-#pragma unroll
-                    for (int i = 0; i < kGroups; ++i) {
-                        now.scale[i] >>= a.scale_bf16 ? 16 : 32;
-                        if (ZERO) now.zero[i] >>= 8;
-                    }
-                    now.bias[0] = now.bias[NT - 1];
-                }
+                for (int m = 0; m < MT; ++m) acc[m] = f32x4{0.f, 0.f, 0.f, 0.f};
+            const int v = tile * 16 + c;
+            u32x4 w = now.w;
+            if (tile >= clear) {                                        // loads that began too early
+                const uint8_t *p = a.codes + (long long)(v < a.V ? v : a.V - 1) * a.code_ld + 16 * g + step * (kStep / 2);
+                if (last >= a.codes && p > last) w = without(w, p - last < 16 ? (uint32_t)(p - last) : 16u);
             }
-            if (G != kStep)
-#pragma unroll
-                for (int n = 0; n < NT; ++n) w[n] = transposed(w[n]);
-            f32x4 part[MT][NT];
+            if (G != kStep) w = transposed(w);
+            f32x4 part[MT];
 #pragma unroll
             for (int t = 0; t < 4; ++t) {                               // 32 units each
                 constexpr int kPer = G / 32;
                 const int grp = t / kPer;
-                f16x8 b[NT];
-#pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    uint32_t z = 8u;
-                    if (ZERO) z = NT == 1 ? now.zero[grp] : n == 1 ? now.zero[grp] >> 8 : now.zero[grp] & 255u;
-                    const f16x2 less = __builtin_bit_cast(f16x2, 0xE400E400u | z * 0x00010001u);
-                    b[n] = eight_codes(w[n][t], less, less + f16x2{(_Float16)960.f, (_Float16)960.f});
-                }
+                const uint32_t z = ZERO ? now.zero[grp] : 8u;
+                const f16x2 less = __builtin_bit_cast(f16x2, 0xE400E400u | z * 0x00010001u);
+                const f16x8 b = eight_codes(w[t], less, less + f16x2{(_Float16)960.f, (_Float16)960.f});
+                const float s = __uint_as_float(a.scale_bf16 ? now.scale[grp] << 16 : now.scale[grp]);
 #pragma unroll
                 for (int m = 0; m < MT; ++m) {
                     const char *at = lds + (size_t)((in_chunk * 4 + t) * MT + m) * TERMS * 1024 + lane * 16;
-                    const f16x8 x1 = *reinterpret_cast<const f16x8 *>(at);
-                    f16x8 x2;
-                    if (TERMS == 2) x2 = *reinterpret_cast<const f16x8 *>(at + 1024);
+                    if (t % kPer == 0) part[m] = f32x4{0.f, 0.f, 0.f, 0.f};
+                    if (TERMS == 2) part[m] = __builtin_amdgcn_mfma_f32_16x16x32_f16(*reinterpret_cast<const f16x8 *>(at + 1024), b, part[m], 0, 0, 0);
+                    part[m] = __builtin_amdgcn_mfma_f32_16x16x32_f16(*reinterpret_cast<const f16x8 *>(at), b, part[m], 0, 0, 0);
+                    if (t % kPer == kPer - 1)
 #pragma unroll
-                    for (int n = 0; n < NT; ++n) {
-                        if (t % kPer == 0) part[m][n] = f32x4{0.f, 0.f, 0.f, 0.f};
-                        if (TERMS == 2) part[m][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x2, b[n], part[m][n], 0, 0, 0);
-                        part[m][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x1, b[n], part[m][n], 0, 0, 0);
-                    }
+                        for (int i = 0; i < 4; ++i) acc[m][i] = __builtin_fmaf(s, part[m][i], acc[m][i]);
                 }
-                if (t % kPer == kPer - 1)
-#pragma unroll
-                    for (int n = 0; n < NT; ++n) {
-                        const uint64_t raw = now.scale[grp];
-                        constexpr bool kPair = NT == 2;
-                        const bool second = kPair && n == 1;
-                        const uint32_t bits = a.scale_bf16 ? (second ? (uint32_t)raw & 0xFFFF0000u : (uint32_t)raw << 16) : (second ? (uint32_t)(raw >> 32) : (uint32_t)raw);
-                        const float s = __uint_as_float(bits);
-#pragma unroll
-                        for (int m = 0; m < MT; ++m)
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) acc[m][n][i] = __builtin_fmaf(s, part[m][n][i], acc[m][n][i]);
-                    }
             }
-            if (step + 1 == steps && v < a.V) {
+            if (step + 1 == steps && v < a.V)
 #pragma unroll
                 for (int m = 0; m < MT; ++m)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const int r = m * 16 + 4 * g + i;
                         if (r >= rows) continue;
-                        const int e = row_exp[r];
-                        float y[NT];
-#pragma unroll
-                        for (int n = 0; n < NT; ++n) y[n] = ldexpf(acc[m][n][i], e) + now.bias[n];
+                        const float y = ldexpf(acc[m][i], row_exp[r]) + now.bias;
                         const long long at = (r0 + r) * a.y_ld + v;
-                        if (NT == 2 && !edge) {
-                            if (a.y_bf16) *reinterpret_cast<u32_any *>(static_cast<uint16_t *>(a.y) + at) = pack_bf16x2(y[0], y[NT - 1]);
-                            else *reinterpret_cast<u64_any *>(static_cast<float *>(a.y) + at) = (uint64_t)__float_as_uint(y[NT - 1]) << 32 | __float_as_uint(y[0]);
-                        } else if (a.y_bf16) static_cast<uint16_t *>(a.y)[at] = (uint16_t)pack_bf16x2(y[0], 0.f);
-                        else static_cast<float *>(a.y)[at] = y[0];
+                        if (a.y_bf16) static_cast<uint16_t *>(a.y)[at] = (uint16_t)pack_bf16x2(y, 0.f);
+                        else static_cast<float *>(a.y)[at] = y;
                     }
-            }
         }
         if (++in_chunk == chunk_steps) in_chunk = 0;
         if (++step == steps) { step = in_chunk = 0; tile += stride; }
@@ -326,18 +265,19 @@ __global__ __launch_bounds__(kThreads, 4) void q4_kernel(Q4Args a, int chunk_ste
     }
 }
 
-template <int TERMS, int MT, int NT, int G, bool ZERO>
+template <int TERMS, int MT, int G, bool ZERO>
 hipError_t launch(const Q4Args &a, hipStream_t stream) {
     static LdsLimit limit;
     const int steps = (a.H + kStep - 1) / kStep, step_bytes = 16 * MT * 2 * TERMS * kStep;
     int chunk = (int)(kLdsRows / step_bytes);
     if (chunk > steps) chunk = steps;
     const size_t bytes = (size_t)chunk * step_bytes;
-    const auto kernel = q4_kernel<TERMS, MT, NT, G, ZERO>;
+    const auto kernel = q4_kernel<TERMS, MT, G, ZERO>;
     const hipError_t e = limit.ensure(reinterpret_cast<const void *>(kernel), bytes);
     if (e != hipSuccess) return e;
-    const int row_blocks = (a.B + 16 * MT - 1) / (16 * MT), tiles = (a.V + 16 * NT - 1) / (16 * NT), groups = (tiles + kWaves - 1) / kWaves;
-    const int resident = kChipGroups * (bytes > 72 * 1024 ? 1 : 2);
+    const int row_blocks = (a.B + 16 * MT - 1) / (16 * MT), tiles = (a.V + 15) / 16, groups = (tiles + kWaves - 1) / kWaves;
+    // workgroups of a compute unit: what its SIMDs' registers and its 160 KB of LDS hold
+    const int by_lds = (int)(158 * 1024 / (bytes + 1024)), by_waves = waves_of(MT, G, ZERO) * 4 / kWaves, resident = kChipGroups * (by_lds < 1 ? 1 : by_lds < by_waves ? by_lds : by_waves);
     for (int y0 = 0; y0 < row_blocks; y0 += 65535) {                    // (a grid has at most that many)
         const int ny = row_blocks - y0 < 65535 ? row_blocks - y0 : 65535;
         int gx = resident / ny;
@@ -353,19 +293,12 @@ hipError_t launch(const Q4Args &a, hipStream_t stream) {
     return hipGetLastError();
 }
 
-// Pairs of tiles where there are few rows, registers for them, and words enough that no wave goes without.
-template <int TERMS, int MT, int G, bool ZERO>
-hipError_t by_words(const Q4Args &a, hipStream_t stream) {
-    if constexpr (MT == 1 && G > 32)
-        if (a.V >= 32 * kWaves * kChipGroups) return launch<TERMS, MT, 2, G, ZERO>(a, stream);
-    return launch<TERMS, MT, 1, G, ZERO>(a, stream);
-}
 template <int TERMS, int MT>
 hipError_t by_group(const Q4Args &a, hipStream_t stream) {
     switch (a.group) {
-        case 32: return a.zero ? by_words<TERMS, MT, 32, true>(a, stream) : by_words<TERMS, MT, 32, false>(a, stream);
-        case 64: return a.zero ? by_words<TERMS, MT, 64, true>(a, stream) : by_words<TERMS, MT, 64, false>(a, stream);
-        default: return a.zero ? by_words<TERMS, MT, 128, true>(a, stream) : by_words<TERMS, MT, 128, false>(a, stream);
+        case 32: return a.zero ? launch<TERMS, MT, 32, true>(a, stream) : launch<TERMS, MT, 32, false>(a, stream);
+        case 64: return a.zero ? launch<TERMS, MT, 64, true>(a, stream) : launch<TERMS, MT, 64, false>(a, stream);
+        default: return a.zero ? launch<TERMS, MT, 128, true>(a, stream) : launch<TERMS, MT, 128, false>(a, stream);
     }
 }
 template <int TERMS>
