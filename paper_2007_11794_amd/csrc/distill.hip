@@ -1,9 +1,13 @@
 // Loss of rows of logits against a teacher's top logits and labels, and its gradient.
 //
-// A row is read once: it stays in the registers of its workgroup from its maximum over its sums to its gradient (what does not fit, of
-// rows beyond kRegs vectors a thread, is read again).  The teacher's words are some tens among tens of thousands: the gradient is
+// A row is read once: it stays in the registers of its workgroup from its maximum over its sums to its gradient (of longer rows a part stays in
+// LDS, and what is left is read again).  The teacher's words are some tens among tens of thousands: the gradient is
 // written as if there were none, and their own places once more behind it, from the logits gathered before.  Where rows are too few
 // to fill the chip they are cut into segments: one launch for a segment's maximum and sums, one that joins them and goes on.
+//
+// What bounds it is memory: 1024 rows of 65536 in bfloat16 with labels, loss and gradient, 68 us = 3.9 TB/s of a copy's 4.8 (up to four exponentials a
+// logit are 27 us of every SIMD's time, beside it); 509 rows of 20011, gradient alone, 15.4 us = 5.3 TB/s; 256 rows of 200000 in fp32 110 us, of which
+// 45 % of a row's bytes are read twice.
 #include "device_utils.h"
 #include "ops.h"
 
