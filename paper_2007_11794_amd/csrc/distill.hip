@@ -31,6 +31,7 @@ struct Exponent {
 };
 
 typedef u32x4 u32x4_any __attribute__((aligned(2)));         // rows may start at any element
+typedef f32x4 f32x4_any __attribute__((aligned(4)));
 
 // Vectors of 16 bytes of a row.
 template <typename Z> struct Row;
@@ -311,7 +312,7 @@ __global__ __launch_bounds__(THREADS, 4) void distill_row_kernel(DistillArgs a, 
     block_reduce<1, false, WAVES>(l, part);
     if (tid == 0) {
         a.loss[n] = row_loss(a, bad, soft_part, hard_part, dead, l[0], logf(s_1) - (z_label - top));
-        *reinterpret_cast<f32x4 *>(a.stats + 4ll * n) = f32x4{top, inv_T, inv_1, 0.f};
+        *reinterpret_cast<f32x4_any *>(a.stats + 4ll * n) = f32x4{top, inv_T, inv_1, 0.f};
     }
     if (!GRAD) return;
     const float g = a.row_weight ? a.row_weight[n] : 1.f;
@@ -492,7 +493,7 @@ __global__ __launch_bounds__(kSegThreads) void distill_segment_kernel(DistillArg
             const float z_minus = wave_sum(hard_part && !bad && label / part_len == lane ? p.label + (some ? d : 0.f) : 0.f);
             if (tid == 0) {
                 a.loss[n] = row_loss(a, bad, soft_part, hard_part, dead, entropy[0] - qz / a.T + q * logf(s_T), logf(s_1) - z_minus);
-                *reinterpret_cast<f32x4 *>(a.stats + 4ll * n) = f32x4{top, inv_T, inv_1, 0.f};
+                *reinterpret_cast<f32x4_any *>(a.stats + 4ll * n) = f32x4{top, inv_T, inv_1, 0.f};
             }
         }
     }

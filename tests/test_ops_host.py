@@ -32,14 +32,14 @@ def test_q4_refusals(change, status):
     assert q4(**change) == status
 
 
-def sample(N=2, V=8, dtype=0, z=at(0), ld=8, T=None, k=None, p=None, m=None, u=at(1024), word=at(2048), lp=at(3072), ws=at(4096), wsb=1 << 15):
+def sample(N=2, V=8, dtype=0, z=at(0), ld=8, T=None, k=None, p=None, m=None, u=at(1024), word=at(2048), lp=at(3328), ws=at(4096), wsb=1 << 15):
     return rn.lib().rnnlm_sample(N, V, dtype, z, ld, T, k, p, m, u, word, lp, ws, wsb, None)
 
 
 @pytest.mark.parametrize("change,status", [
     (dict(N=-1), EINVAL), (dict(V=0), EINVAL), (dict(dtype=2), EINVAL), (dict(ld=7), EINVAL), (dict(z=None), EINVAL), (dict(u=None), EINVAL), (dict(word=None), EINVAL),
     (dict(ws=None), EWORKSPACE), (dict(wsb=8), EWORKSPACE), (dict(ws=at(4100)), EWORKSPACE), (dict(z=at(2)), EINVAL), (dict(u=at(1)), EINVAL), (dict(T=at(1026)), EINVAL),
-    (dict(word=at(0)), EINVAL), (dict(word=at(1024)), EINVAL), (dict(lp=at(2052)), EINVAL), (dict(ws=at(0)), EINVAL), (dict(T=at(2048)), EINVAL), (dict(k=at(3072)), EINVAL),
+    (dict(word=at(0)), EINVAL), (dict(word=at(1024)), EINVAL), (dict(lp=at(2052)), EINVAL), (dict(ws=at(0)), EINVAL), (dict(T=at(2048)), EINVAL), (dict(k=at(3328)), EINVAL),
     (dict(V=(1 << 30) + 1, ld=1 << 31), ERANGE), (dict(N=(1 << 24) + 1), ERANGE), (dict(N=0, z=None, u=None, word=None, ws=None), 0)])
 def test_sample_refusals(change, status):
     assert sample(**change) == status
