@@ -944,7 +944,9 @@ hipError_t launch_row(const SampleArgs &a, int bits, hipStream_t stream) {
 template <typename Z>
 hipError_t launch(const SampleArgs &a, int bits, hipStream_t stream) {
     const int vectors = (a.V + Row<Z>::E - 1) / Row<Z>::E;
-    if (vectors <= 256 * 4) return launch_row<Z, 256, 4>(a, bits, stream);
+    // Four waves a row for short rows, and for any that fit them where there are more rows than compute units.  Us, 256 threads / 1024: a row of 1000
+    // words 11.1 / 13.6; rows of 2853: 141 take 18.6 / 15.0, 600 take 21.3 / 32.0; 256 rows of 4000, top_p, 18.8 / 13.1.
+    if (vectors <= 256 * 4 && (a.V < 2048 || a.N > kChipGroups)) return launch_row<Z, 256, 4>(a, bits, stream);
     if (vectors <= 1024 * 4) return launch_row<Z, 1024, 4>(a, bits, stream);
     if (vectors <= 1024 * 16) return launch_row<Z, 1024, 16>(a, bits, stream);
     const int segments = segments_of<Z>(a.V);
