@@ -308,7 +308,14 @@ hipError_t by_group(const Q4Args &a, hipStream_t stream) {
 }
 template <int TERMS>
 hipError_t by_rows(const Q4Args &a, hipStream_t stream) {
-    return a.B <= 16 ? by_group<TERMS, 1>(a, stream) : a.B <= 32 ? by_group<TERMS, 2>(a, stream) : by_group<TERMS, 4>(a, stream);
+    // Rows of a workgroup: 16 while all their tiles run at once (rows go to LDS by more workgroups), else 32; 64, whose operands need twice the
+    // LDS, where every wave has several tiles and two such workgroups still share a compute unit's LDS and matrix cores (fp32 rows are two products
+    // each).  Us, 16 / 32 / 64 rows: 64 of V=2853 H=400 fp32 7.1 / 9.0 / 15.1; 40 of V=8000 H=1024 14.2 / 18.8 / 30.7; 64 of V=65536 H=512 26.2 / 23.3 / 28.4;
+    // bf16: 64 of V=65536 H=512 23.9 / 19.1 / 21.1; 512 of V=30000 H=512 82.5 / 57.2 / 47.8; 64 of V=100000 H=1024 48.0 / 42.2 / 48.2.
+    const long long tiles = (a.V + 15) / 16, at_once = 2 * kChipGroups * kWaves;
+    if (a.B <= 16 || (a.B + 15) / 16 * tiles <= at_once) return by_group<TERMS, 1>(a, stream);
+    if (a.B > 32 && TERMS * TERMS * a.H <= 512 && (a.B + 63) / 64 * tiles >= 2 * at_once) return by_group<TERMS, 4>(a, stream);
+    return by_group<TERMS, 2>(a, stream);
 }
 
 }  // namespace

@@ -67,6 +67,23 @@ def test_many_words(B, V, H, group):
     check(d, call(d))
 
 
+@pytest.mark.parametrize("B,V,H", [(17, 33001, 96), (33, 22003, 33), (47, 30010, 130), (100, 10007, 260), (33, 131085, 64), (70, 65553, 129), (200, 32771, 100)])
+@pytest.mark.parametrize("x,y,group,zero", [("f32", "f32", 32, True), ("f32", "f32", 64, False), ("f32", "f32", 128, True), ("bf16", "bf16", 32, False), ("bf16", "f32", 64, True),
+                                            ("bf16", "bf16", 128, False)])
+def test_many_rows_of_many_words(B, V, H, x, y, group, zero):
+    """Sizes at which a workgroup takes 32 or 64 rows.  Rows at the blocks' edges are compared."""
+    d = make(B, V, H, group, x=x, zero=zero, pad=V % 3)
+    check(d, call(d, y), rows=[b for b in (0, 15, 16, 31, 32, 63, 64, 99, 127, 128, 199, B - 1) if b < B])
+
+
+def test_rows_of_larger_blocks_do_not_depend_on_each_other():
+    for x in ("f32", "bf16"):
+        d = make(70, 65601, 64, 32, x=x)
+        whole = call(d)
+        for b in (0, 31, 32, 64, 69):
+            assert torch.equal(call(d, x=d["x"][b:b + 1])[0], whole[b])
+
+
 @pytest.mark.parametrize("pad,shift", [(0, 0), (1, 0), (0, 1), (3, 2), (14, 0), (14, 6), (30, 16), (62, 9)])
 @pytest.mark.parametrize("H", [34, 100, 260])
 def test_rows_of_codes_anywhere(pad, shift, H):
