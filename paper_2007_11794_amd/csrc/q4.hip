@@ -10,8 +10,8 @@
 // those four lanes (four register swaps) turns "32 units of one group per lane" into "the same group in all four lanes", so that a matrix
 // instruction never mixes two groups, whatever their size.  The A operand, the rows, lies in LDS in operand order, staged once per workgroup.
 //
-// What bounds it: V = 1048576, H = 1024, 1 row in 123 us is 4.6 TB/s, what a copy reaches.  Shorter launches (V = 200000, H = 1024, 16 rows, zero points 43.6
-// us, 2.7 TB/s; V = 65536, H = 512, 1 row 9.7 us) are the way to the first products (launch, rows to LDS and their magnitudes, 5 us), and
+// What bounds it: V = 1048576, H = 1024, 1 row in 123 us is 4.6 TB/s, what a copy reaches.  Shorter launches (V = 200000, H = 1024, 16 rows, zero points 41.2
+// us, 2.9 TB/s; V = 65536, H = 512, 1 row 9.1 us) are the way to the first products (launch, rows to LDS and their magnitudes, 4 us), and
 // a last round of tiles that some waves have none of; a step costs a wave some 100 vector instructions for 2 KB of codes, half the time memory
 // takes for them.  Two tiles a wave, sharing the reads of the rows' operands, had fewer waves in flight: 47.2 us for the first of these.
 #include "device_utils.h"
@@ -24,6 +24,7 @@ namespace {
 constexpr int kThreads = 512, kWaves = kThreads / 64;
 constexpr int kStep = 128;                                   // units of a step: 16 bytes of codes a lane
 constexpr size_t kLdsRows = 144 * 1024;                      // most LDS for the rows' operands
+constexpr int kHeld = 4;                                     // eights of a thread that wait in registers while the rows' magnitudes are found
 
 // Waves of a SIMD: as many as keep their requests in registers.  V = 1000000, H = 256, groups of 128, 1 row: 4 waves 42.8 us, 6 waves 37.9; groups
 // of 32, H = 100, 8 rows: 33.9 / 38.1.
@@ -34,25 +35,40 @@ typedef u32x4 u32x4_any __attribute__((aligned(1)));         // rows of codes ma
 
 typedef f32x4 f32x4_any __attribute__((aligned(4)));
 
-// Elements k .. k + 7 of a row of H, 0 behind it.
-__device__ __forceinline__ void eight_of_row(const void *x, long long at, int k, int H, bool bf16, float (&out)[8]) {
-    if (k + 8 <= H) {
-        if (bf16) {
-            const u32x4 v = *reinterpret_cast<const u32x4_any *>(static_cast<const uint16_t *>(x) + at + k);
+// Elements k .. k + 7 of a row of H, 0 behind it, as they come from memory (so that several can be on their way).
+template <bool BF16>
+struct Eight {
+    u32x4 w[BF16 ? 1 : 2] = {};
+    __device__ __forceinline__ void load(const void *x, long long at, int k, int H) {
+        if (BF16) {
+            const uint16_t *p = static_cast<const uint16_t *>(x) + at + k;
+            if (k + 8 <= H) w[0] = *reinterpret_cast<const u32x4_any *>(p);
+            else
 #pragma unroll
-            for (int i = 0; i < 4; ++i) { out[2 * i] = __uint_as_float(v[i] << 16); out[2 * i + 1] = __uint_as_float(v[i] & 0xFFFF0000u); }
+                for (int i = 0; i < 8; ++i) w[0][i >> 1] |= k + i < H ? (uint32_t)p[i] << (16 * (i & 1)) : 0;
         } else {
-            const float *p = static_cast<const float *>(x) + at + k;
-            const f32x4 a = *reinterpret_cast<const f32x4_any *>(p), b = *reinterpret_cast<const f32x4_any *>(p + 4);
+            const uint32_t *p = static_cast<const uint32_t *>(x) + at + k;
+            if (k + 8 <= H) {
+                w[0] = *reinterpret_cast<const u32x4_any *>(p);
+                w[BF16 ? 0 : 1] = *reinterpret_cast<const u32x4_any *>(p + 4);
+            } else
 #pragma unroll
-            for (int i = 0; i < 4; ++i) { out[i] = a[i]; out[4 + i] = b[i]; }
+                for (int i = 0; i < 8; ++i) w[BF16 ? 0 : i >> 2][i & 3] = k + i < H ? p[i] : 0;
         }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            out[i] = k + i >= H ? 0.f : bf16 ? bf16_to_f32(static_cast<const uint16_t *>(x)[at + k + i]) : static_cast<const float *>(x)[at + k + i];
     }
-}
+    __device__ __forceinline__ float operator[](int i) const {
+        if (BF16) return __uint_as_float(i & 1 ? w[0][i >> 1] & 0xFFFF0000u : w[0][i >> 1] << 16);
+        return __uint_as_float(w[BF16 ? 0 : i >> 2][i & 3]);
+    }
+    __device__ __forceinline__ uint32_t top(uint32_t t) const {            // the largest finite magnitude, and t
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const uint32_t m = __float_as_uint((*this)[i]) & 0x7FFFFFFFu;
+            if (m < 0x7F800000u && m > t) t = m;
+        }
+        return t;
+    }
+};
 
 // What a wave needs of one step of a tile of 16 words, as it comes from memory.
 template <int GROUPS, bool ZERO>
@@ -162,48 +178,69 @@ __global__ __launch_bounds__(kThreads, waves_of(MT, G, ZERO)) void q4_kernel(Q4A
     request(q[0]);
     request(q[1]);                                                      // on their way while the rows are staged
 
-    // The power of two of every row: its largest finite magnitude goes to [2^14, 2^15).
-    for (int r = tid; r < kRows; r += kThreads) row_top[r] = 0;
-    __syncthreads();
-    for (int i = tid; i < kRows * steps * 16; i += kThreads) {
-        const int r = i % kRows, k = i / kRows * 8;
-        if (r >= rows || k >= a.H) continue;
-        float x[8];
-        eight_of_row(a.x, (r0 + r) * a.x_ld, k, a.H, a.x_bf16, x);
-        uint32_t top = 0;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const uint32_t m = __float_as_uint(x[j]) & 0x7FFFFFFFu;
-            if (m < 0x7F800000u && m > top) top = m;
-        }
-        atomicMax(&row_top[r], top);
-    }
-    __syncthreads();
-    for (int r = tid; r < kRows; r += kThreads) row_exp[r] = row_top[r] ? ilogbf(__uint_as_float(row_top[r])) - 14 : 0;
-    __syncthreads();
     // First unit of lane group g in product t of 32 units: as the codes are where a step is one group, else with the codes transposed.
     auto unit_of = [](int t, int g) { return G == kStep ? t / 4 * kStep + 32 * g + t % 4 * 8 : 32 * t + 8 * g; };
+    // Eights of units in operand order; a thread's, kThreads apart, are of one row.
+    const int my_row = wave % MT * 16 + c;
+    auto load = [&](Eight<TERMS == 1> &x, int i, int k0, int n) {
+        const int k = k0 + unit_of((i >> 6) / MT, g);
+        if (i < n / 32 * MT * 64 && my_row < rows && k < a.H) x.load(a.x, (r0 + my_row) * a.x_ld, k, a.H);
+    };
+    auto put = [&](const Eight<TERMS == 1> &x, int i, int n, int e) {
+        if (i >= n / 32 * MT * 64) return;
+        const int frag = i >> 6;
+        f16x8 t1, t2;
+#pragma unroll
+        for (int s = 0; s < 8; ++s) {
+            const float y = ldexpf(x[(s >> 1) + 4 * (s & 1)], -e);
+            t1[s] = (_Float16)y;
+            t2[s] = (_Float16)(fabsf(y) < INFINITY ? y - (float)t1[s] : 0.f);       // (a NaN is in the first term)
+        }
+        *reinterpret_cast<f16x8 *>(lds + (size_t)frag * TERMS * 1024 + lane * 16) = t1;
+        if (TERMS == 2) *reinterpret_cast<f16x8 *>(lds + (size_t)frag * 2048 + 1024 + lane * 16) = t2;
+    };
+    // The power of two of every row: its largest finite magnitude goes to [2^14, 2^15).  Rows that are kHeld eights a thread are requested at
+    // once and stay in registers meanwhile; of longer ones each eight is read for the magnitude and again.  (Read twice, 1 row of V = 65536, H = 1024
+    // took 15.4 us for 14.0, bf16 14.4 for 12.3.)
+    const int units = steps * kStep, eights = units / 32 * MT * 64;
+    const bool held = eights <= kHeld * kThreads && chunk_steps >= steps;
+    Eight<TERMS == 1> x[kHeld];
+    if (held)
+#pragma unroll
+        for (int j = 0; j < kHeld; ++j) load(x[j], tid + j * kThreads, 0, units);
+    for (int r = tid; r < kRows; r += kThreads) row_top[r] = 0;
+    __syncthreads();
+    uint32_t top = 0;
+    if (held) {
+#pragma unroll
+        for (int j = 0; j < kHeld; ++j) top = x[j].top(top);
+    } else {
+        for (int i = tid; i < eights; i += kThreads) {
+            Eight<TERMS == 1> one;
+            load(one, i, 0, units);
+            top = one.top(top);
+        }
+    }
+    atomicMax(&row_top[my_row], top);
+    __syncthreads();
+    auto exponent_of = [&](int r) { return row_top[r] ? ilogbf(__uint_as_float(row_top[r])) - 14 : 0; };
+    for (int r = tid; r < kRows; r += kThreads) row_exp[r] = exponent_of(r);
+    const int my_exp = exponent_of(my_row);
+    if (held)
+#pragma unroll
+        for (int j = 0; j < kHeld; ++j) put(x[j], tid + j * kThreads, units, my_exp);
+    __syncthreads();
     auto stage = [&](int k0, int n) {                                   // units k0 .. k0 + n - 1
         for (int i = tid; i < n / 32 * MT * 64; i += kThreads) {
-            const int frag = i >> 6, l = i & 63, r = (frag % MT) * 16 + (l & 15), k = k0 + unit_of(frag / MT, l >> 4);
-            float x[8] = {};
-            if (r < rows) eight_of_row(a.x, (r0 + r) * a.x_ld, k, a.H, a.x_bf16, x);
-            const int e = row_exp[r];
-            f16x8 t1, t2;
-#pragma unroll
-            for (int s = 0; s < 8; ++s) {
-                const float y = ldexpf(x[(s >> 1) + 4 * (s & 1)], -e);
-                t1[s] = (_Float16)y;
-                t2[s] = (_Float16)(fabsf(y) < INFINITY ? y - (float)t1[s] : 0.f);       // (a NaN is in the first term)
-            }
-            *reinterpret_cast<f16x8 *>(lds + (size_t)frag * TERMS * 1024 + l * 16) = t1;
-            if (TERMS == 2) *reinterpret_cast<f16x8 *>(lds + (size_t)frag * 2048 + 1024 + l * 16) = t2;
+            Eight<TERMS == 1> one;
+            load(one, i, k0, n);
+            put(one, i, n, my_exp);
         }
     };
 
     f32x4 acc[MT];
     int tile = blockIdx.x * kWaves + wave, step = 0, left = rounds * steps, in_chunk = 0;
-    bool staged = false;
+    bool staged = held;
     auto body = [&](Codes<kGroups, ZERO> &now, Codes<kGroups, ZERO> &free) {
         if (in_chunk == 0 && !(staged && chunk_steps >= steps)) {       // (the same in all waves)
             if (staged) __syncthreads();                                // the chunk before has been read
