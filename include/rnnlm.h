@@ -388,7 +388,7 @@ int rnnlm_pack_ids(const uint32_t *ctx_idx, const uint32_t *small_lm_idx, int N,
  * Codes less their zero are exact; an fp32 x is taken as two fp16 terms relative to its row's largest finite magnitude (good to
  * 2^-23 of itself or 2^-39 of that magnitude, whichever is larger); sums are held in fp32, and y is rounded once at the end.
  * An x that is infinite or NaN reaches the outputs of its row as in exact arithmetic (infinity times a zero weight is NaN),
- * and no other row.  B = 0 is a no-op.  H <= 65536, V <= 2^30.
+ * and no other row.  B = 0 is a no-op.  H <= 65536, V <= 2^30, B <= 2^24 (RNNLM_ERANGE).
  */
 int rnnlm_q4_matvec(int B, int V, int H, int group, const uint8_t *codes, long long code_ld, int scale_dtype, const void *scale,
                     const uint8_t *zero_or_null, const float *bias_or_null, int x_dtype, const void *x, long long x_ld,
@@ -427,7 +427,7 @@ size_t rnnlm_sample_workspace_bytes(int N, int V);
  *   temperature  dev f32[N] or NULL: 1;  top_k dev i32[N] or NULL: all;  top_p dev f32[N] or NULL: 1;  min_p dev f32[N] or NULL: 0
  *   u            dev f32[N]
  *   word         dev i32[N] out;  logprob dev f32[N] out or NULL
- * N = 0 is a no-op.  V <= 2^30.
+ * N = 0 is a no-op.  V <= 2^30, N <= 2^21 (RNNLM_ERANGE).
  */
 int rnnlm_sample(int N, int V, int dtype, const void *logits, long long ld, const float *temperature_or_null,
                  const int32_t *top_k_or_null, const float *top_p_or_null, const float *min_p_or_null, const float *u,
@@ -456,7 +456,7 @@ size_t rnnlm_distill_workspace_bytes(int N, int V);
  * teacher's word that the student cannot say makes the loss infinite.  Loss and gradient of a row are NaN where a word or label
  * is outside [0, V) (and not -1), a teacher's logit is NaN or +infinity, or, in a row with a part, a logit is NaN or
  * +infinity or none is finite.
- * N = 0 is a no-op; K = 0 is labels only.  V <= 2^30, K <= RNNLM_DISTILL_MAX_K (RNNLM_ERANGE).
+ * N = 0 is a no-op; K = 0 is labels only.  V <= 2^30, N <= 2^21, K <= RNNLM_DISTILL_MAX_K (RNNLM_ERANGE).
  */
 #define RNNLM_DISTILL_MAX_K 4096
 int rnnlm_distill(int N, int V, int K, int dtype, const void *logits, long long ld, const int32_t *teacher_word,

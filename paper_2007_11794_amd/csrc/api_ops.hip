@@ -12,6 +12,7 @@ namespace {
 bool known_dtype(int dtype) { return dtype == RNNLM_F32 || dtype == RNNLM_BF16; }
 size_t size_of(int dtype) { return dtype == RNNLM_BF16 ? 2 : 4; }
 constexpr int kMaxWords = 1 << 30, kMaxUnits = 1 << 16, kMaxRows = 1 << 24;
+constexpr int kMaxGroups = 1 << 21;                  // rows that take a workgroup each: a grid holds fewer than 2^32 threads
 constexpr long long kMaxStride = 1ll << 40;          // rows * stride stays in 64 bits
 
 // `rows` rows of `row` bytes, `stride` bytes apart.
@@ -45,14 +46,16 @@ bool overlap(const Range (&ins)[NI], const Range (&outs)[NO]) {
 bool aligned(const void *p, size_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
 
 int check_distill(int N, int V, int K, int dtype, const void *logits, long long ld, const int32_t *teacher_word, const float *teacher_logit,
-                  const int32_t *label, float T, float a, const void *grad, long long grad_ld) {
+                  const int32_t *label, float T, float a, const float *row_weight, const void *grad, long long grad_ld) {
     if (N < 0 || V <= 0 || K < 0 || !known_dtype(dtype)) return RNNLM_EINVAL;
-    if (V > kMaxWords || N > kMaxRows || K > RNNLM_DISTILL_MAX_K) return RNNLM_ERANGE;
+    if (V > kMaxWords || N > kMaxGroups || K > RNNLM_DISTILL_MAX_K) return RNNLM_ERANGE;
     if (ld < V || ld > kMaxStride || (grad && (grad_ld < V || grad_ld > kMaxStride))) return RNNLM_EINVAL;
     if (!(T > 0.f) || !std::isfinite(T) || !(a >= 0.f && a <= 1.f) || (!label && a != 0.f)) return RNNLM_EINVAL;
     if (N == 0) return RNNLM_OK;
     if (!logits || (K > 0 && (!teacher_word || !teacher_logit))) return RNNLM_EINVAL;
-    if (!aligned(logits, size_of(dtype)) || !aligned(grad, size_of(dtype))) return RNNLM_EINVAL;
+    if (!aligned(logits, size_of(dtype)) || !aligned(grad, size_of(dtype)) || !aligned(teacher_word, 4) || !aligned(teacher_logit, 4) ||
+        !aligned(label, 4) || !aligned(row_weight, 4))
+        return RNNLM_EINVAL;
     return RNNLM_OK;
 }
 
@@ -116,7 +119,7 @@ size_t rnnlm_sample_workspace_bytes(int N, int V) { return N <= 0 || V <= 0 ? 0 
 int rnnlm_sample(int N, int V, int dtype, const void *logits, long long ld, const float *temperature, const int32_t *top_k, const float *top_p,
                  const float *min_p, const float *u, int32_t *word, float *logprob, void *workspace, size_t workspace_bytes, void *hip_stream) {
     if (N < 0 || V <= 0 || !known_dtype(dtype)) return RNNLM_EINVAL;
-    if (V > kMaxWords || N > kMaxRows) return RNNLM_ERANGE;
+    if (V > kMaxWords || N > kMaxGroups) return RNNLM_ERANGE;
     if (ld < V || ld > kMaxStride) return RNNLM_EINVAL;
     if (N == 0) return RNNLM_OK;
     if (!logits || !u || !word) return RNNLM_EINVAL;
@@ -137,7 +140,7 @@ size_t rnnlm_distill_workspace_bytes(int N, int V) { return N <= 0 || V <= 0 ? 0
 int rnnlm_distill(int N, int V, int K, int dtype, const void *logits, long long ld, const int32_t *teacher_word, const float *teacher_logit,
                   const int32_t *label, float temperature, float label_weight, const float *row_weight, float *loss, float *stats, void *grad,
                   long long grad_ld, void *workspace, size_t workspace_bytes, void *hip_stream) {
-    const int rc = check_distill(N, V, K, dtype, logits, ld, teacher_word, teacher_logit, label, temperature, label_weight, grad, grad_ld);
+    const int rc = check_distill(N, V, K, dtype, logits, ld, teacher_word, teacher_logit, label, temperature, label_weight, row_weight, grad, grad_ld);
     if (rc != RNNLM_OK || N == 0) return rc;
     if (!loss || !stats || !aligned(loss, 4) || !aligned(stats, 4)) return RNNLM_EINVAL;
     const size_t need = distill_workspace_bytes(N, V), es = size_of(dtype), nk = (size_t)N * K * 4;
@@ -158,7 +161,7 @@ int rnnlm_distill(int N, int V, int K, int dtype, const void *logits, long long 
 int rnnlm_distill_backward(int N, int V, int K, int dtype, const void *logits, long long ld, const int32_t *teacher_word,
                            const float *teacher_logit, const int32_t *label, float temperature, float label_weight, const float *row_weight,
                            const float *stats, void *grad, long long grad_ld, void *hip_stream) {
-    const int rc = check_distill(N, V, K, dtype, logits, ld, teacher_word, teacher_logit, label, temperature, label_weight, grad, grad_ld);
+    const int rc = check_distill(N, V, K, dtype, logits, ld, teacher_word, teacher_logit, label, temperature, label_weight, row_weight, grad, grad_ld);
     if (rc != RNNLM_OK || N == 0) return rc;
     if (!grad || !stats || !aligned(stats, 4)) return RNNLM_EINVAL;
     const size_t es = size_of(dtype), nk = (size_t)N * K * 4;

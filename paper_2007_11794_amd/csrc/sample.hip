@@ -950,7 +950,7 @@ hipError_t launch(const SampleArgs &a, int bits, hipStream_t stream) {
     if (vectors <= 1024 * 4) return launch_row<Z, 1024, 4>(a, bits, stream);
     if (vectors <= 1024 * 16) return launch_row<Z, 1024, 16>(a, bits, stream);
     const int segments = segments_of<Z>(a.V);
-    if ((long long)a.N * segments > 0x7FFFFFFF) return hipErrorInvalidValue;
+    if ((long long)a.N * segments > 0x7FFFFFFF / kSegThreads) return hipErrorInvalidValue;     // (more than 2^37 logits)
     const int groups = a.N * segments;
     static LdsLimit limit;
     constexpr size_t pick_bytes = sizeof(Shared<kLongBins, 1>) + (size_t)kLongHeld * 8;

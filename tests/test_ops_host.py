@@ -153,3 +153,13 @@ def test_interleaved_rows_are_no_overlap():
     assert distill(z=at(0), ld=16, grad=at(28), gld=16, ws=at(4096)) == EINVAL
     assert distill(z=at(0), ld=16, grad=at(68), gld=16, ws=at(4096)) == EINVAL
     assert distill(z=at(0), ld=16, grad=at(32), gld=17, ws=at(4096)) == EINVAL
+
+
+@pytest.mark.parametrize("change,status", [(dict(tw=at(1025)), EINVAL), (dict(tl=at(1282)), EINVAL), (dict(label=at(1537), a=0.5), EINVAL), (dict(g=at(1795)), EINVAL),
+                                           (dict(N=(1 << 21) + 1), ERANGE)])
+def test_distill_refuses_misaligned_lists_and_too_many_rows(change, status):
+    assert distill(**change) == status
+
+
+def test_sample_refuses_more_rows_than_a_grid_holds():
+    assert sample(N=(1 << 21) + 1) == ERANGE
