@@ -83,6 +83,20 @@ def test_many_rows(V):
     check(logits(N, V, 6, torch.bfloat16), u, T, k, p, m)
 
 
+@pytest.mark.parametrize("V,dtype", [(2047, torch.float32), (2049, torch.float32), (3001, torch.float32), (4096, torch.float32), (3001, torch.bfloat16), (8190, torch.bfloat16)])
+def test_words_do_not_depend_on_how_many_rows_are_drawn(V, dtype):
+    """More rows than compute units and a few of them go to workgroups of different sizes."""
+    N = 300
+    u, T, k, p, m = limits(N, V, V)
+    z = logits(N, V, V + 1, dtype)
+    check(z, u, T, k, p, m)
+    word, lp = draw(z, u, T, k, p, m)
+    for n in range(0, N, 60):
+        at = slice(n, n + 7)
+        few, few_lp = draw(z[at], u[at], T[at], k[at], p[at], m[at])
+        assert (few == word[at]).all() and np.array_equal(few_lp, lp[at], equal_nan=True)
+
+
 @pytest.mark.parametrize("V", [7, 700, 33000, 140000])
 def test_rows_of_few_values(V):
     """Hundreds of words of one logit at every border."""
