@@ -10,8 +10,8 @@
 // those four lanes (four register swaps) turns "32 units of one group per lane" into "the same group in all four lanes", so that a matrix
 // instruction never mixes two groups, whatever their size.  The A operand, the rows, lies in LDS in operand order, staged once per workgroup.
 //
-// What bounds it: V = 1048576, H = 1024, 1 row in 123 us is 4.6 TB/s, what a copy reaches.  Shorter launches (V = 200000, H = 1024, 16 rows, zero points 41.2
-// us, 2.9 TB/s; V = 65536, H = 512, 1 row 9.1 us) are the way to the first products (launch, rows to LDS and their magnitudes, 4 us), and
+// What bounds it: V = 1048576, H = 1024, 1 row in 123 us is 4.6 TB/s, what a copy reaches.  Shorter launches (V = 200000, H = 1024, 16 rows, zero points 37
+// us, 3.2 TB/s; V = 65536, H = 512, 1 row 9.1 us) are the way to the first products (launch, rows to LDS and their magnitudes, 4 us), and
 // a last round of tiles that some waves have none of; a step costs a wave some 100 vector instructions for 2 KB of codes, half the time memory
 // takes for them.  Two tiles a wave, sharing the reads of the rows' operands, had fewer waves in flight: 47.2 us for the first of these.
 #include "device_utils.h"
@@ -26,9 +26,10 @@ constexpr int kStep = 128;                                   // units of a step:
 constexpr size_t kLdsRows = 144 * 1024;                      // most LDS for the rows' operands
 constexpr int kHeld = 4;                                     // eights of a thread that wait in registers while the rows' magnitudes are found
 
-// Waves of a SIMD: as many as keep their requests in registers.  V = 1000000, H = 256, groups of 128, 1 row: 4 waves 42.8 us, 6 waves 37.9; groups
-// of 32, H = 100, 8 rows: 33.9 / 38.1.
-constexpr int waves_of(int MT, int G, bool zero) { return MT == 1 && (G == 128 || (G == 64 && !zero)) ? 6 : 4; }
+// Waves of a SIMD: six where their requests fit 80 registers, which is to say where there are few scales, no zero points, or rows of one term.  Us, four
+// waves / six: V = 1000000, H = 256, groups of 128, 1 row 42.8 / 37.9; H = 100, groups of 32, 8 rows 33.2 / 30.5; V = 200000, H = 1024, groups of 64 with
+// zero points, 16 rows in bf16 40.8 / 37, in fp32 44.6 / 45.7.
+constexpr int waves_of(int TERMS, int MT, int G, bool zero) { return MT == 1 && (G == 128 || !zero || (G == 64 && TERMS == 1)) ? 6 : 4; }
 
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef u32x4 u32x4_any __attribute__((aligned(1)));         // rows of codes may start anywhere
@@ -117,7 +118,7 @@ __device__ __forceinline__ u32x4 without(u32x4 w, uint32_t n) {
 }
 
 template <int TERMS, int MT, int G, bool ZERO>
-__global__ __launch_bounds__(kThreads, waves_of(MT, G, ZERO)) void q4_kernel(Q4Args a, int chunk_steps, int rounds) {
+__global__ __launch_bounds__(kThreads, waves_of(TERMS, MT, G, ZERO)) void q4_kernel(Q4Args a, int chunk_steps, int rounds) {
     constexpr int kRows = 16 * MT, kGroups = kStep / G;
     extern __shared__ __attribute__((aligned(1024))) char lds[];        // [units of a chunk / 32][MT][TERMS][64 lanes][8]
     __shared__ uint32_t row_top[kRows];                                 // the row's largest finite magnitude
@@ -296,6 +297,10 @@ __global__ __launch_bounds__(kThreads, waves_of(MT, G, ZERO)) void q4_kernel(Q4A
         }
         if (++in_chunk == chunk_steps) in_chunk = 0;
         if (++step == steps) { step = in_chunk = 0; tile += stride; }
+        // (the same in all lanes, which the compiler does not see)
+        in_chunk = __builtin_amdgcn_readfirstlane(in_chunk);
+        step = __builtin_amdgcn_readfirstlane(step);
+        tile = __builtin_amdgcn_readfirstlane(tile);
     };
     while (true) {                                                      // the three sets of codes in turn, so that none is ever copied
         body(q[0], q[2]);
@@ -319,7 +324,7 @@ hipError_t launch(const Q4Args &a, hipStream_t stream) {
     if (e != hipSuccess) return e;
     const int row_blocks = (a.B + 16 * MT - 1) / (16 * MT), tiles = (a.V + 15) / 16, groups = (tiles + kWaves - 1) / kWaves;
     // workgroups of a compute unit: what its SIMDs' registers and its 160 KB of LDS hold
-    const int by_lds = (int)(158 * 1024 / (bytes + 1024)), by_waves = waves_of(MT, G, ZERO) * 4 / kWaves, resident = kChipGroups * (by_lds < 1 ? 1 : by_lds < by_waves ? by_lds : by_waves);
+    const int by_lds = (int)(158 * 1024 / (bytes + 1024)), by_waves = waves_of(TERMS, MT, G, ZERO) * 4 / kWaves, resident = kChipGroups * (by_lds < 1 ? 1 : by_lds < by_waves ? by_lds : by_waves);
     for (int y0 = 0; y0 < row_blocks; y0 += 65535) {                    // (a grid has at most that many)
         const int ny = row_blocks - y0 < 65535 ? row_blocks - y0 : 65535;
         int gx = resident / ny;
