@@ -35,6 +35,11 @@ struct SampleArgs {
     void *ws;
 };
 size_t sample_workspace_bytes(int N, int V);
+// Words that can be listed of a row in segments.  In bfloat16 a bin is one logit, and some hundredth of the words may have it.
+__host__ __device__ constexpr int long_list(int V) { return V / 16 > 8192 ? V / 16 : 8192; }
+// Does the launch that draws keep the list in LDS?  `listed` counts the words that there are, and may be more than the list's length.
+constexpr int kLongHeld = 12288;
+__host__ __device__ constexpr bool list_in_lds(int listed, int V) { return listed <= long_list(V) && listed <= kLongHeld; }
 hipError_t launch_sample(const SampleArgs &a, hipStream_t stream);
 
 struct DistillArgs {

@@ -664,16 +664,13 @@ __global__ __launch_bounds__(THREADS, 4) void sample_row_kernel(SampleArgs a, in
 
 // ---- rows in segments
 
-constexpr int kSegThreads = 256, kSegWaves = kSegThreads / 64, kSegVectors = 16, kLongHeld = 12288, kLongBins = 4096, kPickThreads = 1024;
+constexpr int kSegThreads = 256, kSegWaves = kSegThreads / 64, kSegVectors = 16, kLongBins = 4096, kPickThreads = 1024;
 template <typename Z> __host__ __device__ constexpr int segment_words() { return kSegThreads * kSegVectors * Row<Z>::E; }
 // Words of a wave's part of the segment that word `from` begins, as Words lays them out.
 template <typename Z> __device__ __forceinline__ int part_words(int V, int from) {
     const int len = min(V - from, segment_words<Z>());
     return ((len + Row<Z>::E - 1) / Row<Z>::E + kSegThreads - 1) / kSegThreads * 64 * Row<Z>::E;
 }
-
-// Words that can be listed of a row in memory.  In bfloat16 a bin is one logit, and some hundredth of the words may have it.
-__host__ __device__ constexpr int long_list(int V) { return V / 16 > 8192 ? V / 16 : 8192; }
 
 // Of one row in the workspace, behind its histogram of kLongBins weights (or counts): the deciding bin and what is wanted of it, the words listed,
 // how many there are, of every segment its maximum, and of every wave's quarter of one the weight of its words that are kept for certain.
@@ -855,9 +852,10 @@ __global__ __launch_bounds__(kPickThreads, 4) void sample_pick_kernel(SampleArgs
     };
     const bool all = lists_all(l, V), of_bin = lists_bin(l, V);
     const int listed = all || of_bin ? *r.listed : 0;
+    const bool fits = listed <= long_list(V);                 // (too many are counted on, but not listed)
     // (several passes go over the list: it stays in LDS where it fits)
     const u64 *list = r.list;
-    if (listed <= kLongHeld) {
+    if (list_in_lds(listed, V)) {
         for (int i = tid; i < listed; i += kPickThreads) held[i] = r.list[i];
         list = held;
         __syncthreads();
@@ -879,7 +877,6 @@ __global__ __launch_bounds__(kPickThreads, 4) void sample_pick_kernel(SampleArgs
             }
         }
     };
-    const bool fits = listed <= long_list(V);
     u64 total;
     if (!fits || (all || of_bin ? false : l.few(V))) {
         total = search.all_steps(l, V, over_row);
