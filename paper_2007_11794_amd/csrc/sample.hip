@@ -52,19 +52,22 @@ __device__ __forceinline__ double fma_with(double a, double b, double c) {
 }
 
 // 2^y for y <= 0 as a whole number of 2^-bits, to nearest (bits <= 50; anything below -200 is nothing).  2^f on [-1/2, 1/2] is 1 + f times a polynomial fitted for the
-// least relative error, 8.1e-13 (which moves a border between two words by that share of the sum).  Sums and products alone, at full rate: the nearest whole number n comes of adding 1.5 * 2^52 and taking it
-// off, its power of two goes into the exponent, and the result is rounded by adding 2^52, below which the last bit counts 1 (with the
-// instructions for rounding, conversion and scaling, a quarter of that rate each, 65536 weights took a workgroup 17.7 us for this).
+// least relative error: with the rounding of its steps 3.3e-16 = 2^-51.4, so that a weight is off by less than one unit of 2^-50, whatever f.  (A degree less is good to
+// 1.5e-14, 17 of those units, two to 8.1e-13, and a border between two words moves by that share of the sum.)  Sums and products alone, at full rate: the nearest whole number
+// n comes of adding 1.5 * 2^52 and taking it off, its power of two goes into the exponent, and the result is rounded by adding 2^52, below which the last
+// bit counts 1 (with the instructions for rounding, conversion and scaling, a quarter of that rate each, 65536 weights took a workgroup 17.7 us for this).
 __device__ __forceinline__ u64 fixed_exp2(double y, int bits) {
     y = fmax(y, -200.0);
     const double t = y + 0x1.8p52, f = y - (t - 0x1.8p52);
-    double q = fma_with(0x1.61c4f05b35904p-20, f, 0x1.00d8538df1462p-16);
-    q = fma_with(q, f, 0x1.430aa8842f4a4p-13);
-    q = fma_with(q, f, 0x1.5d874d067423fp-10);
-    q = fma_with(q, f, 0x1.3b2ab5ed6e014p-7);
-    q = fma_with(q, f, 0x1.c6b08dced3e72p-5);
-    q = fma_with(q, f, 0x1.ebfbdff8edeaap-3);
-    q = fma_with(q, f, 0x1.62e42fef89d19p-1);
+    double q = fma_with(0x1.e3a9369210e0ap-28, f, 0x1.b671b4e00fe0ap-24);
+    q = fma_with(q, f, 0x1.62c1478e7a2f7p-20);
+    q = fma_with(q, f, 0x1.ffcb58c80dfbap-17);
+    q = fma_with(q, f, 0x1.4309126c04a5fp-13);
+    q = fma_with(q, f, 0x1.5d87fe9b8fd28p-10);
+    q = fma_with(q, f, 0x1.3b2ab6fbd6d25p-7);
+    q = fma_with(q, f, 0x1.c6b08d703e172p-5);
+    q = fma_with(q, f, 0x1.ebfbdff82c431p-3);
+    q = fma_with(q, f, 0x1.62e42fefa3a12p-1);
     q = fma(q, f, 1.0);
     const uint32_t n = (uint32_t)__double_as_longlong(t) + (uint32_t)bits;
     const u64 x = (u64)__double_as_longlong(q) + ((u64)(n << 20) << 32);

@@ -3,7 +3,7 @@ import numpy as np
 import pytest
 import torch
 
-from test_gpu_sample import check
+from test_gpu_sample import check, draw
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -22,3 +22,27 @@ def test_more_words_of_one_logit_than_a_list_holds(V, dtype, tied):
     check(z, u, p=[0.9, 0.2, 0.6])
     check(z, u, k=[40, 4000, 2000], p=[0.5, 0.9, 0.7])
     check(z[:1], u[1:2], p=[0.5])
+
+
+def near_halves(T, count, low, high, seed):
+    """z1, z2 (float32) whose weights e^(z / T) add up to 1 but for something between `low` and `high` in magnitude, and that."""
+    rng = np.random.default_rng(seed)
+    found = []
+    while sum(len(f[0]) for f in found) < count:
+        z1 = (T * rng.uniform(-2.0, -0.3, 1 << 20)).astype(np.float32)
+        z2 = (T * np.log1p(-np.exp(z1.astype(np.float64) / T))).astype(np.float32)
+        off = np.exp(z1.astype(np.float64) / T) - (1 - np.exp(z2.astype(np.float64) / T))
+        at = (np.abs(off) >= low) & (np.abs(off) <= high)
+        found.append((z1[at], z2[at], off[at]))
+    return [np.concatenate([f[i] for f in found])[:count] for i in range(3)]
+
+
+@pytest.mark.parametrize("T", [1.0, 0.75, 2.5])
+def test_weights_are_good_to_the_last_bit_of_their_numbers(T):
+    """Three words, the first of weight 1, at u = 1/2: it is drawn where the others weigh less than it.  Their weights are off by a unit of 2^-50 each
+    at most, 1.8e-15 together (and the definition here by 2e-16 each), which a difference of 4e-15 and more has to survive."""
+    z1, z2, off = near_halves(T, 150, 4e-15, 2e-13, int(T * 100))
+    N = len(z1)
+    z = torch.from_numpy(np.stack([np.zeros(N, np.float32), z1, z2], 1)).to(DEV)
+    word, _ = draw(z, np.full(N, 0.5, np.float32), T=np.full(N, T))
+    assert np.array_equal(word, np.where(off < 0, 0, 1)), int((word != np.where(off < 0, 0, 1)).sum())
