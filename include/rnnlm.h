@@ -422,7 +422,8 @@ size_t rnnlm_sample_workspace_bytes(int N, int V);
  * +infinity, those share the row equally.  A row without any word (all -infinity), with a NaN, or with a
  * temperature that is negative or not finite, u outside [0, 1), or top_p or min_p NaN gets word -1 and logprob NaN.
  * Weights are fixed-point numbers of min(50, 62 - ceil(log2 V)) fractional bits, computed in 64 bits (off by less than one unit of the
- * last of them) and added exactly: the word does not depend on how the work is split.  (Words of a weight that rounds to nothing there are never drawn.)
+ * last of them) and added exactly: the word does not depend on how the work is split.  (Words of a weight that rounds to nothing there are
+ * never drawn; min_p is compared with these numbers.)
  *   logits       dev [N][ld] float or bfloat16
  *   temperature  dev f32[N] or NULL: 1;  top_k dev i32[N] or NULL: all;  top_p dev f32[N] or NULL: 1;  min_p dev f32[N] or NULL: 0
  *   u            dev f32[N]

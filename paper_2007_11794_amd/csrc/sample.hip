@@ -540,9 +540,10 @@ __device__ __forceinline__ float log_share(u64 w, u64 total) { return (float)log
 // that has it, of its lanes, of the lane's words.  target_of(their weight) is what the sum has to pass.
 template <int THREADS, typename W, typename S, typename F>
 __device__ __forceinline__ u64 draw_from_registers(const W &words, S &sh, const Scale &scale, const Limits &l, u64 border, int from, F target_of) {
-    // no word below it is kept (by min_p: of a weight of `least` at least, with a hundredth of a factor of two for what logarithm and bound are off)
+    // No word below it is kept.  (By min_p: of a number of `least` at least, which half a unit less is rounded to, with a hundredth of a factor of
+    // two for what logarithm and bound are off.)
     float floor_z = border ? logit_of(border) : -INFINITY;
-    if (scale.least) floor_z = fmaxf(floor_z, (float)(scale.high + ((double)log2f(fminf(l.mp, 1.f)) - 0.01) / scale.per) - 1e-6f * fabsf(scale.top));
+    if (scale.least) floor_z = fmaxf(floor_z, (float)(scale.high + ((double)log2f((float)scale.least - 0.5f) - scale.bits - 0.01) / scale.per) - 1e-6f * fabsf(scale.top));
     floor_z = uniform(floor_z);
     auto weigh = [&](int i, const float (&z)[4], u64 (&w)[4]) {
         u64 s = 0;

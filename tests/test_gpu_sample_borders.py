@@ -46,3 +46,24 @@ def test_weights_are_good_to_the_last_bit_of_their_numbers(T):
     z = torch.from_numpy(np.stack([np.zeros(N, np.float32), z1, z2], 1)).to(DEV)
     word, _ = draw(z, np.full(N, 0.5, np.float32), T=np.full(N, T))
     assert np.array_equal(word, np.where(off < 0, 0, 1)), int((word != np.where(off < 0, 0, 1)).sum())
+
+
+@pytest.mark.parametrize("V,dtype", [(1000, torch.float32), (5000, torch.float32), (5000, torch.bfloat16), (60000, torch.float32), (70000, torch.float32), (200003, torch.float32),
+                                     (200003, torch.bfloat16)])
+def test_a_min_p_of_one_unit(V, dtype):
+    """All words but one weigh between half a unit of the weights' numbers and one, and are rounded to what min_p asks for, far from any that weighs
+    more: what is drawn does not depend on which others a wave has beside them."""
+    bits = min(50, 62 - int(np.ceil(np.log2(V))))
+    low = (-np.log(2.0) * (bits + torch.linspace(0.05, 0.9, 16))).to(dtype)
+    low = low[(-low.double() / np.log(2.0) > bits + 0.03) & (-low.double() / np.log(2.0) < bits + 0.92)][0]
+    z = torch.full((4, V), float(low), device=DEV, dtype=dtype)
+    z[:, V - 3] = 0.0
+    z[1, :700] = -float("inf")
+    u = [0.0, 0.0, 0.5, 2.0 ** -24]
+    word, lp = draw(z, u, m=np.full(4, 2.0 ** -bits))
+    assert list(word[:3]) == [0, 700, V - 3]
+    total = 2.0 ** bits + np.array([V - 1, V - 701, V - 1])
+    want = np.log(np.array([1.0, 1.0, 2.0 ** bits]) / total)
+    assert (np.abs(lp[:3] - want) <= 2.0 ** -23 * np.abs(want) + 2.0 ** -50).all()
+    first = 2.0 ** -24 * (2.0 ** bits + V - 1)                     # the numbers up to the word that is drawn have to pass it
+    assert word[3] == (V - 3 if first >= V - 3 else int(first))
