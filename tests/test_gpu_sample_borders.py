@@ -3,7 +3,8 @@ import numpy as np
 import pytest
 import torch
 
-from test_gpu_sample import check, draw
+from ops_reference import sample_row
+from test_gpu_sample import check, draw, limits, logits
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -67,3 +68,20 @@ def test_a_min_p_of_one_unit(V, dtype):
     assert (np.abs(lp[:3] - want) <= 2.0 ** -23 * np.abs(want) + 2.0 ** -50).all()
     first = 2.0 ** -24 * (2.0 ** bits + V - 1)                     # the numbers up to the word that is drawn have to pass it
     assert word[3] == (V - 3 if first >= V - 3 else int(first))
+
+
+@pytest.mark.parametrize("V", [1, 2, 3, 64, 1000, 4096])
+def test_log_probabilities_of_short_rows(V):
+    """The weights' unit is 2^-50 here, however few words there are; a row of one word has nothing to be off by."""
+    N = 40
+    z = logits(N, V, 7 * V + 1)
+    u, T, k, p, m = limits(N, V, V + 2)
+    word, lp = draw(z, u, T, k, p, m)
+    one, rows = 2.0 ** -50, z.double().cpu().numpy()
+    at = lambda x, n: np.float64(np.float32(x[n]))  # noqa: E731
+    for n in range(N):
+        want, want_lp, w = sample_row(rows[n], at(u, n), at(T, n), int(k[n]), at(p, n), at(m, n))
+        # rounded once to 32 bits; the word's number and the kept words' (V at most, each at least as heavy as what it is off by) a unit each
+        assert word[n] == want and abs(lp[n] - want_lp) <= 2.0 ** -24 * abs(want_lp) + one / w + V * one, (n, lp[n], want_lp)
+    if V == 1:
+        assert (word == 0).all() and (lp == 0).all()
