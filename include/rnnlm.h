@@ -405,7 +405,7 @@ int rnnlm_q4_matvec(int B, int V, int H, int group, const uint8_t *codes, long l
  */
 int rnnlm_q4_quantize(int V, int H, int group, const float *w, uint8_t *codes, float *scale, uint8_t *zero_or_null);
 
-/* Bytes of workspace rnnlm_sample needs (0 for N <= 0 or V <= 0). */
+/* Bytes of workspace rnnlm_sample needs for N rows of V words, or fewer of either (0 for N <= 0 or V <= 0). */
 size_t rnnlm_sample_workspace_bytes(int N, int V);
 
 /*
@@ -434,7 +434,7 @@ int rnnlm_sample(int N, int V, int dtype, const void *logits, long long ld, cons
                  const int32_t *top_k_or_null, const float *top_p_or_null, const float *min_p_or_null, const float *u,
                  int32_t *word, float *logprob_or_null, void *workspace, size_t workspace_bytes, void *hip_stream);
 
-/* Bytes of workspace rnnlm_distill needs (0 for N <= 0 or V <= 0). */
+/* Bytes of workspace rnnlm_distill needs for N rows of V words, or fewer of either (0 for N <= 0 or V <= 0). */
 size_t rnnlm_distill_workspace_bytes(int N, int V);
 
 /*

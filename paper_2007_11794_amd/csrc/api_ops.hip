@@ -135,7 +135,7 @@ int rnnlm_sample(int N, int V, int dtype, const void *logits, long long ld, cons
     return launch_sample(a, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? RNNLM_OK : RNNLM_EDEVICE;
 }
 
-size_t rnnlm_distill_workspace_bytes(int N, int V) { return N <= 0 || V <= 0 ? 0 : distill_workspace_bytes(N, V); }
+size_t rnnlm_distill_workspace_bytes(int N, int V) { return N <= 0 || V <= 0 ? 0 : distill_workspace_most(N, V); }
 
 int rnnlm_distill(int N, int V, int K, int dtype, const void *logits, long long ld, const int32_t *teacher_word, const float *teacher_logit,
                   const int32_t *label, float temperature, float label_weight, const float *row_weight, float *loss, float *stats, void *grad,

@@ -8,6 +8,8 @@
 // What bounds it is memory: 1024 rows of 65536 in bfloat16 with labels, loss and gradient, 68 us = 3.9 TB/s of a copy's 4.8 (up to four exponentials a
 // logit are 27 us of every SIMD's time, beside it); 509 rows of 20011, gradient alone, 15.4 us = 5.3 TB/s; 256 rows of 200000 in fp32 110 us, of which
 // 45 % of a row's bytes are read twice.
+#include <algorithm>
+
 #include "device_utils.h"
 #include "ops.h"
 
@@ -576,8 +578,9 @@ Cut cut_row(int V, int E, int segments) {
 // Rows too few to fill the chip by one workgroup each, and so long that one compute unit's way to memory (some 80 GB/s) takes longer than a
 // second launch.  Steps, us, a workgroup a row / segments: fp32, V = 65536: 1 row 14.7 / 13.2, 16 rows 15.3 / 13.1, 64 rows 18.0 / 18.5, 100 rows
 // 19.1 / 25.3; V = 200000: 100 rows 55.7 / 75.4; V = 20000: 8 rows 10.1 / 13.1, the loss alone 9.1 / 12.2.
+constexpr int kFewRows = 48;
 int segments_of(int N, int V, bool bf16) {
-    if (N > 48 || (long long)V * (bf16 ? 2 : 4) < 192 * 1024) return 1;
+    if (N > kFewRows || (long long)V * (bf16 ? 2 : 4) < 192 * 1024) return 1;
     int s = 2 * kChipGroups / N;
     if (s > V / 4096) s = V / 4096;
     return s < 2 ? 1 : s > kMaxSegments ? kMaxSegments : s;
@@ -619,6 +622,11 @@ hipError_t backward(const DistillArgs &a, hipStream_t stream) {
 size_t distill_workspace_bytes(int N, int V) {
     const int s = segments_of(N, V, false);                 // (bfloat16 has no more)
     return s > 1 ? (size_t)N * s * sizeof(Part) : 16;
+}
+size_t distill_workspace_most(int N, int V) {               // (segments_of() does not fall with V)
+    size_t most = 16;
+    for (int n = 1; n <= N && n <= kFewRows; ++n) most = std::max(most, distill_workspace_bytes(n, V));
+    return most;
 }
 
 hipError_t launch_distill(const DistillArgs &a, hipStream_t stream) { return a.bf16 ? forward<uint16_t>(a, stream) : forward<float>(a, stream); }

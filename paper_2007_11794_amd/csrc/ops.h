@@ -58,7 +58,8 @@ struct DistillArgs {
     long long grad_ld;
     void *ws;
 };
-size_t distill_workspace_bytes(int N, int V);
+size_t distill_workspace_bytes(int N, int V);   // of this call
+size_t distill_workspace_most(int N, int V);    // of any call of no more rows and words
 hipError_t launch_distill(const DistillArgs &a, hipStream_t stream);
 hipError_t launch_distill_backward(const DistillArgs &a, hipStream_t stream);
 
