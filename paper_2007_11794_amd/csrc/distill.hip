@@ -364,7 +364,7 @@ __global__ __launch_bounds__(THREADS, 4) void distill_row_kernel(DistillArgs a, 
 }
 
 // ---- rows in segments
-constexpr int kSegThreads = 256, kSegWaves = kSegThreads / 64, kMaxSegments = 64;
+constexpr int kSegThreads = kDistillThreads, kSegWaves = kSegThreads / 64, kMaxSegments = 64;
 // Of one segment: maximum m, sums relative to it at both temperatures, sum of q (z - m) and of q over the teacher's words in it, the label's
 // z - m.
 struct Part { float m, s_T, s_1, qz, q, label, pad[2]; };
@@ -563,16 +563,9 @@ hipError_t launch_segments(const DistillArgs &a, int parts, int part_len, int se
     const hipError_t e = limit.ensure(reinterpret_cast<const void *>(kernel), bytes);
     if (e != hipSuccess) return e;
     const long long groups = (long long)a.N * segments;
-    if (groups > 0x7FFFFFFF) return hipErrorInvalidValue;
+    if (groups > kDistillGroups) return hipErrorInvalidValue;
     kernel<<<(unsigned)groups, kSegThreads, bytes, stream>>>(a, parts, part_len, segments, seg_len, hash_size_of(a.K));
     return hipGetLastError();
-}
-
-// Segments of a row: how many, and their length (a multiple of a vector).
-struct Cut { int segments, len; };
-Cut cut_row(int V, int E, int segments) {
-    const int vectors = (V + E - 1) / E, per = (vectors + segments - 1) / segments;
-    return Cut{(vectors + per - 1) / per, per * E};
 }
 
 // Rows too few to fill the chip by one workgroup each, and so long that one compute unit's way to memory (some 80 GB/s) takes longer than a
@@ -613,7 +606,7 @@ hipError_t forward(const DistillArgs &a, hipStream_t stream) {
 
 template <typename Z>
 hipError_t backward(const DistillArgs &a, hipStream_t stream) {
-    const Cut cut = cut_row(a.V, Row<Z>::E, (a.V + 8191) / 8192);
+    const Cut cut = cut_for_backward(a.N, a.V, Row<Z>::E);
     return form_of(a) == kTwo ? launch_segments<Z, true, true>(a, 0, 1, cut.segments, cut.len, stream) : launch_segments<Z, true, false>(a, 0, 1, cut.segments, cut.len, stream);
 }
 

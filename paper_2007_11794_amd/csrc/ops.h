@@ -60,6 +60,19 @@ struct DistillArgs {
 };
 size_t distill_workspace_bytes(int N, int V);   // of this call
 size_t distill_workspace_most(int N, int V);    // of any call of no more rows and words
+// Segments of a row: how many, and their length (a multiple of a vector of E elements).
+struct Cut { int segments, len; };
+inline Cut cut_row(int V, int E, int segments) {
+    const int vectors = (V + E - 1) / E, per = (vectors + segments - 1) / segments;
+    return Cut{(vectors + per - 1) / per, per * E};
+}
+// Of the gradient alone: some 8192 words each, and more where a grid of fewer than 2^32 threads would not hold as many workgroups.
+constexpr int kDistillThreads = 256;
+constexpr long long kDistillGroups = 0xFFFFFFFFll / kDistillThreads;
+inline Cut cut_for_backward(int N, int V, int E) {
+    const int segments = (V + 8191) / 8192;
+    return cut_row(V, E, segments * (long long)N <= kDistillGroups ? segments : (int)(kDistillGroups / N));
+}
 hipError_t launch_distill(const DistillArgs &a, hipStream_t stream);
 hipError_t launch_distill_backward(const DistillArgs &a, hipStream_t stream);
 
