@@ -18,11 +18,11 @@ namespace rnnlm {
 namespace {
 
 // e^(x / T), per = log2(e) / T in two floats: what rounding the exponent's argument loses goes into a first-order term, so that shares
-// of any size are good to some 2^-22 of themselves.
+// of any size are good to some 2^-22 of themselves.  (Below T = 2^-127 per would be infinite, and 0 times it NaN.)
 struct Exponent {
     float per, rest;
     __device__ explicit Exponent(float T) {
-        const double c = 1.4426950408889634 / (double)T;
+        const double c = 1.4426950408889634 / fmax((double)T, 0x1p-127);
         per = (float)c;
         rest = (float)(c - (double)per);
     }
@@ -192,11 +192,12 @@ __device__ __forceinline__ void write_listed(const DistillArgs &a, const List &l
     if (threadIdx.x == 0 && !in_list && label >= from && label < from + len && k_1 != 0.f) Row<Z>::put(out + label, grad(z_label) - k_1);
 }
 
-// loss of a row: soft = sum q (log q - log p), the label's -log p
+// Loss of a row: soft = T sum q (log q - log p), the label's -log p.  (That sum grows as 1 / T and T^2 passes the range of a float far in front of
+// what their product is.)
 __device__ __forceinline__ float row_loss(const DistillArgs &a, bool bad, bool soft_part, bool hard_part, bool dead, float soft, float hard) {
     if (bad || ((soft_part || hard_part) && dead)) return quiet_nan();
     float l = 0.f;
-    if (soft_part) l = (1.f - a.a) * a.T * a.T * soft;
+    if (soft_part) l = (1.f - a.a) * (a.T * soft);
     if (hard_part) l += a.a * hard;
     return l;
 }
@@ -307,7 +308,7 @@ __global__ __launch_bounds__(THREADS, 4) void distill_row_kernel(DistillArgs a, 
         for (int k = tid; k < a.K; k += THREADS) {
             if (list.word[k] < 0) continue;
             const float d = list.q[k] - t_top, q = exponent.fine(d) / t_sum;
-            if (q > 0.f) l[0] += q * (d / a.T - log_t - (list.z[k] - top) / a.T + log_sum);
+            if (q > 0.f) l[0] += q * (d - (list.z[k] - top) + a.T * (log_sum - log_t));
             list.q[k] = q;
         }
     }
@@ -470,7 +471,7 @@ __global__ __launch_bounds__(kSegThreads) void distill_segment_kernel(DistillArg
         for (int k = tid; k < a.K; k += kSegThreads) {
             if (list.word[k] < 0) continue;
             const float d = list.q[k] - t_top, q = exponent.fine(d) / t_sum;
-            if (q > 0.f) entropy[0] += q * (d / a.T - log_t);
+            if (q > 0.f) entropy[0] += q * (d - a.T * log_t);
             list.q[k] = q;
         }
     }
@@ -494,7 +495,7 @@ __global__ __launch_bounds__(kSegThreads) void distill_segment_kernel(DistillArg
             const float qz = wave_sum(p.q > 0.f ? p.qz + p.q * d : 0.f), q = wave_sum(p.q);
             const float z_minus = wave_sum(hard_part && !bad && label / part_len == lane ? p.label + (some ? d : 0.f) : 0.f);
             if (tid == 0) {
-                a.loss[n] = row_loss(a, bad, soft_part, hard_part, dead, entropy[0] - qz / a.T + q * logf(s_T), logf(s_1) - z_minus);
+                a.loss[n] = row_loss(a, bad, soft_part, hard_part, dead, entropy[0] - qz + q * (a.T * logf(s_T)), logf(s_1) - z_minus);
                 *reinterpret_cast<f32x4_any *>(a.stats + 4ll * n) = f32x4{top, inv_T, inv_1, 0.f};
             }
         }

@@ -1,9 +1,11 @@
 """Distillation at the borders of its forms, workspaces and numbers, against the definition in 64 bits."""
+import numpy as np
 import pytest
 import torch
 
 import paper_2007_11794_amd as rn
-from test_gpu_distill import case, check
+from ops_reference import distill_row
+from test_gpu_distill import backward, case, check, run
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -19,3 +21,23 @@ def test_a_workspace_of_many_rows_serves_the_last_few():
         rn.rnnlm_distill(d["z"], d["words"], d["t"], loss, stats, ws, temperature=2.0, labels=d["label"], label_weight=0.25, row_weight=d["g"], grad=grad)
         torch.cuda.synchronize()
         check(d, 2.0, 0.25, loss, grad, rows=range(0, N, 12))
+
+
+@pytest.mark.parametrize("T", [1e-45, 1e-40, 4e-39, 1e-38, 1e-30, 1e-20, 1e-10, 1e10, 1e18])
+@pytest.mark.parametrize("N,V", [(6, 3000), (2, 70001), (60, 70001)])
+def test_temperatures_of_any_size(N, V, T):
+    """A loss of T times something of order one: where that is below the normal numbers, its two last roundings are half a least step, 2^-150, each."""
+    t = float(np.float32(T))
+    for a in (0.0, 0.25):
+        d = case(N, V, 40)
+        loss, stats, grad = run(d, T, a)
+        only = run(d, T, a, grad=False)[0]
+        wanted = torch.full((N,), np.nan, dtype=torch.float64)
+        for n in range(0, N, 10):
+            want, _, far = distill_row(d["z"][n].double().cpu().numpy(), d["words"][n].cpu().numpy(), d["t"][n].double().cpu().numpy(), int(d["label"][n]), t, a)
+            r = 2.0 ** -18 + (V / 256 + 16) * 2.0 ** -24
+            bar = (t * t * (1 - a) + a) * (r + 2.0 ** -20 * far) + 2.0 ** -22 * abs(want) + 2 * 2.0 ** -150
+            assert abs(float(loss[n]) - want) <= bar and abs(float(only[n]) - want) <= bar, (n, float(loss[n]), float(only[n]), want)
+            wanted[n] = want
+        check(d, T, a, wanted, grad, rows=range(0, N, 10))
+        check(d, T, a, wanted, backward(d, T, a, stats), rows=range(0, N, 10))
