@@ -550,11 +550,15 @@ hipError_t launch_row_kernel(const DistillArgs &a, hipStream_t stream) {
     return hipGetLastError();
 }
 template <typename Z, int THREADS, int R, int STASH>
-hipError_t launch_rows(const DistillArgs &a, hipStream_t stream) {
+hipError_t launch_steps(const DistillArgs &a, hipStream_t stream) {           // (loss and gradient)
     const Form form = form_of(a);
-    if (!a.grad) return form == kOne ? launch_row_kernel<Z, THREADS, R, 0, false, kOne>(a, stream) : launch_row_kernel<Z, THREADS, R, 0, false, kTwoSums>(a, stream);
     if (form == kOne) return launch_row_kernel<Z, THREADS, R, STASH, true, kOne>(a, stream);
     return form == kTwo ? launch_row_kernel<Z, THREADS, R, STASH, true, kTwo>(a, stream) : launch_row_kernel<Z, THREADS, R, STASH, true, kTwoSums>(a, stream);
+}
+template <typename Z, int THREADS, int R>
+hipError_t launch_rows(const DistillArgs &a, hipStream_t stream) {
+    if (a.grad) return launch_steps<Z, THREADS, R, 0>(a, stream);
+    return form_of(a) == kOne ? launch_row_kernel<Z, THREADS, R, 0, false, kOne>(a, stream) : launch_row_kernel<Z, THREADS, R, 0, false, kTwoSums>(a, stream);
 }
 template <typename Z, bool BACKWARD, bool TWO>
 hipError_t launch_segments(const DistillArgs &a, int parts, int part_len, int segments, int seg_len, hipStream_t stream) {
@@ -563,9 +567,7 @@ hipError_t launch_segments(const DistillArgs &a, int parts, int part_len, int se
     const auto kernel = distill_segment_kernel<Z, BACKWARD, TWO>;
     const hipError_t e = limit.ensure(reinterpret_cast<const void *>(kernel), bytes);
     if (e != hipSuccess) return e;
-    const long long groups = (long long)a.N * segments;
-    if (groups > kDistillGroups) return hipErrorInvalidValue;
-    kernel<<<(unsigned)groups, kSegThreads, bytes, stream>>>(a, parts, part_len, segments, seg_len, hash_size_of(a.K));
+    kernel<<<(unsigned)a.N * segments, kSegThreads, bytes, stream>>>(a, parts, part_len, segments, seg_len, hash_size_of(a.K));
     return hipGetLastError();
 }
 
@@ -598,11 +600,11 @@ hipError_t forward(const DistillArgs &a, hipStream_t stream) {
     const int vectors = (a.V + E - 1) / E;
     // The fewest waves that hold a row, for as many rows at once as the chip takes.  Us, this size / the next: 2000 rows of 1500 14.8 / 25.8, 2000 of 4000 18.1 /
     // 27.5, 200 of 4000 10.0 / 10.1; 500 of 16000 16.0 / 17.8, 2000 of 10000 40.2 / 50.7; 500 of 32000 29.2 / 37.2, 60 of 32000 11.6 / 13.8.
-    if (vectors <= 256 * 4) return launch_rows<Z, 256, 4, 0>(a, stream);
-    if (vectors <= 512 * 8) return launch_rows<Z, 512, 8, 0>(a, stream);
-    if (vectors <= 512 * 16) return launch_rows<Z, 512, 16, 0>(a, stream);
-    if (vectors <= 1024 * 16 || !a.grad || list_bytes(a.K) > 28 * 1024) return launch_rows<Z, 1024, 16, 0>(a, stream);
-    return launch_rows<Z, 1024, E == 4 ? 20 : 16, 8>(a, stream);
+    if (vectors <= 256 * 4) return launch_rows<Z, 256, 4>(a, stream);
+    if (vectors <= 512 * 8) return launch_rows<Z, 512, 8>(a, stream);
+    if (vectors <= 512 * 16) return launch_rows<Z, 512, 16>(a, stream);
+    if (vectors <= 1024 * 16 || !a.grad || list_bytes(a.K) > 28 * 1024) return launch_rows<Z, 1024, 16>(a, stream);
+    return launch_steps<Z, 1024, E == 4 ? 20 : 16, 8>(a, stream);
 }
 
 template <typename Z>
