@@ -1,5 +1,6 @@
 // C ABI of the operators that take no model: argument checks in front of the launches, and the 4-bit quantiser (host code).
 #include <math.h>
+#include <stdint.h>
 
 #include <algorithm>
 
@@ -13,7 +14,10 @@ bool known_dtype(int dtype) { return dtype == RNNLM_F32 || dtype == RNNLM_BF16; 
 size_t size_of(int dtype) { return dtype == RNNLM_BF16 ? 2 : 4; }
 constexpr int kMaxWords = 1 << 30, kMaxUnits = 1 << 16, kMaxRows = 1 << 24;
 constexpr int kMaxGroups = 1 << 21;                  // rows that take a workgroup each: a grid holds fewer than 2^32 threads
-constexpr long long kMaxStride = 1ll << 40;          // rows * stride stays in 64 bits
+constexpr long long kMaxStride = 1ll << 40;
+// Can `rows` rows of n elements of es bytes lie `ld` elements apart?  Their bytes have to be a number of 63 bits, which offsets and the search for
+// shared bytes count on.
+bool strides(long long rows, long long n, long long ld, size_t es) { return ld >= n && ld <= kMaxStride && (rows <= 1 || ld <= INT64_MAX / (long long)es / rows); }
 
 // `rows` rows of `row` bytes, `stride` bytes apart.
 struct Range {
@@ -49,7 +53,7 @@ int check_distill(int N, int V, int K, int dtype, const void *logits, long long 
                   const int32_t *label, float T, float a, const float *row_weight, const void *grad, long long grad_ld) {
     if (N < 0 || V <= 0 || K < 0 || !known_dtype(dtype)) return RNNLM_EINVAL;
     if (V > kMaxWords || N > kMaxGroups || K > RNNLM_DISTILL_MAX_K) return RNNLM_ERANGE;
-    if (ld < V || ld > kMaxStride || (grad && (grad_ld < V || grad_ld > kMaxStride))) return RNNLM_EINVAL;
+    if (!strides(N, V, ld, size_of(dtype)) || (grad && !strides(N, V, grad_ld, size_of(dtype)))) return RNNLM_EINVAL;
     if (!(T > 0.f) || !std::isfinite(T) || !(a >= 0.f && a <= 1.f) || (!label && a != 0.f)) return RNNLM_EINVAL;
     if (N == 0) return RNNLM_OK;
     if (!logits || (K > 0 && (!teacher_word || !teacher_logit))) return RNNLM_EINVAL;
@@ -70,7 +74,7 @@ int rnnlm_q4_matvec(int B, int V, int H, int group, const uint8_t *codes, long l
     if (!known_dtype(scale_dtype) || !known_dtype(x_dtype) || !known_dtype(y_dtype)) return RNNLM_EINVAL;
     if (V > kMaxWords || H > kMaxUnits || B > kMaxRows) return RNNLM_ERANGE;
     const long long row = (H + 1) / 2, groups = (H + group - 1) / group;
-    if (code_ld < row || code_ld > kMaxStride || x_ld < H || x_ld > kMaxStride || y_ld < V || y_ld > kMaxStride) return RNNLM_EINVAL;
+    if (!strides(V, row, code_ld, 1) || !strides(B, H, x_ld, size_of(x_dtype)) || !strides(B, V, y_ld, size_of(y_dtype))) return RNNLM_EINVAL;
     if (B == 0) return RNNLM_OK;
     if (!codes || !scale || !x || !y) return RNNLM_EINVAL;
     if (!aligned(scale, size_of(scale_dtype)) || !aligned(x, size_of(x_dtype)) || !aligned(y, size_of(y_dtype)) || !aligned(bias, 4)) return RNNLM_EINVAL;
@@ -120,7 +124,7 @@ int rnnlm_sample(int N, int V, int dtype, const void *logits, long long ld, cons
                  const float *min_p, const float *u, int32_t *word, float *logprob, void *workspace, size_t workspace_bytes, void *hip_stream) {
     if (N < 0 || V <= 0 || !known_dtype(dtype)) return RNNLM_EINVAL;
     if (V > kMaxWords || N > kMaxGroups) return RNNLM_ERANGE;
-    if (ld < V || ld > kMaxStride) return RNNLM_EINVAL;
+    if (!strides(N, V, ld, size_of(dtype))) return RNNLM_EINVAL;
     if (N == 0) return RNNLM_OK;
     if (!logits || !u || !word) return RNNLM_EINVAL;
     if (!aligned(logits, size_of(dtype)) || !aligned(temperature, 4) || !aligned(top_k, 4) || !aligned(top_p, 4) || !aligned(min_p, 4) ||
