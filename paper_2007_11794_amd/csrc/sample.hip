@@ -160,28 +160,31 @@ struct Limits {
 // Weights and bins of a row whose maximum is known.
 struct Scale {
     double high, per;                                         // the maximum; log2(e) / temperature
-    float top, bin_scale;
+    float top, half_top, bin_scale;                           // bin_scale: bins for half the distance (the whole of it may pass the range of a float)
     int bits, last_bin;
     bool alike;                                               // a maximum of +infinity: those words are 0 here, all others -infinity
     u64 least;                                                // min_p's weight
     __device__ Scale(const Limits &l, float maximum, int bits, int bins) : bits(bits), last_bin(bins - 1) {
         alike = maximum == INFINITY;
         top = alike ? 0.f : maximum;
+        half_top = 0.5f * top;
         high = uniform((double)top);
         per = uniform(1.4426950408889634 / (double)l.T);
-        bin_scale = uniform(fminf((float)(per * ((double)bins / kOctaves)), 3.4e38f));
+        bin_scale = uniform(fminf((float)(per * (2.0 * bins / kOctaves)), 3.4e38f));
         least = l.mp > 0.f ? uniform((u64)ceil((double)fminf(l.mp, 1.f) * (double)(1ull << bits))) : 0;
     }
     __device__ __forceinline__ float seen(float z) const { return !alike ? z : z == INFINITY ? 0.f : -INFINITY; }
     __device__ __forceinline__ u64 weight(float z) const { return fixed_exp2(((double)z - high) * per, bits); }
     // Bounds of the logits in a bin and, for the lower one, in those in front of it, with room for the rounding of bin_of.
     __device__ __forceinline__ float lowest(int bin) const {
-        return fmaxf(uniform(top - (float)(bin + 1) / bin_scale * (1.f + 0x1p-20f) - 0x1p-20f * fabsf(top)), -__FLT_MAX__);
+        return fmaxf(uniform(__builtin_fmaf(-2.f, (float)(bin + 1) * (1.f + 0x1p-20f) / bin_scale, top) - 0x1p-20f * fabsf(top)), -__FLT_MAX__);
     }
-    __device__ __forceinline__ float highest(int bin) const { return uniform(top - (float)bin / bin_scale * (1.f - 0x1p-20f) + 0x1p-20f * fabsf(top)); }
+    __device__ __forceinline__ float highest(int bin) const {
+        return uniform(__builtin_fmaf(-2.f, (float)bin * (1.f - 0x1p-20f) / bin_scale, top) + 0x1p-20f * fabsf(top));
+    }
     // rises as z falls; what is in the last one weighs nothing
     __device__ __forceinline__ int bin_of(float z) const {
-        const float x = (top - z) * bin_scale;
+        const float x = __builtin_fmaf(-0.5f, z, half_top) * bin_scale;
         return x < (float)last_bin ? (int)x : last_bin;
     }
 };

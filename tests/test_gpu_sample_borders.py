@@ -85,3 +85,18 @@ def test_log_probabilities_of_short_rows(V):
         assert word[n] == want and abs(lp[n] - want_lp) <= 2.0 ** -24 * abs(want_lp) + one / w + V * one, (n, lp[n], want_lp)
     if V == 1:
         assert (word == 0).all() and (lp == 0).all()
+
+
+@pytest.mark.parametrize("V,dtype", [(300, torch.float32), (5000, torch.float32), (5000, torch.bfloat16), (70000, torch.float32), (140000, torch.bfloat16)])
+@pytest.mark.parametrize("T", [2e37, 1e38, 3e38])
+def test_logits_further_apart_than_the_largest_number(V, dtype, T):
+    """At such a temperature they weigh something all the same, and have an order."""
+    rng = np.random.default_rng(V)
+    z = torch.from_numpy((rng.uniform(-1, 1, (8, V)) * 3.3e38).astype(np.float32)).to(DEV).to(dtype)
+    z[:, 5] = 3.3e38
+    u, T = rng.random(8).astype(np.float32) * np.float32(0.99999), np.full(8, T)
+    k, p = np.geomspace(2, V - 1, 8).astype(int), np.array([0.02, 0.1, 0.3, 0.5, 0.7, 0.9, 0.99, 0.999])
+    check(z, u, T=T)
+    check(z, u, T=T, k=k)
+    check(z, u, T=T, p=p)
+    check(z, u, T=T, k=k, p=p, m=p / 100)
