@@ -2,8 +2,9 @@
 //
 // Few rows: the codes are read once, half a byte for every weight, and everything else has to keep out of their way.  A code less
 // its zero is a small whole number, exact in fp16, so the matrix cores take it as it is, and the scale goes onto the fp32 sum of its
-// group: no weight is ever rounded.  An fp32 x is two fp16 terms relative to its row's largest magnitude (two products instead of one), a
-// bf16 x is one.
+// group: no weight is ever rounded.  An fp32 x is two fp16 terms relative to its row's largest magnitude (two products instead of one), the second times
+// 2^11, so that a unit next to one 2^28 times as large still has its 23 bits (relative to that one it is good to 2^-50; as the first term's last bits, 2^-39);
+// a bf16 x is one.
 //
 // One wave takes 16 words by 16 * MT rows.  Its B operand (16x16x32: lane = word, 8 units) comes straight from memory: a
 // lane loads 16 bytes, 32 consecutive codes of its word, the four lanes of a word 64 consecutive bytes; a transpose of 4 x 4 dwords over
@@ -120,6 +121,11 @@ __device__ __forceinline__ u32x4 without(u32x4 w, uint32_t n) {
 template <int TERMS, int MT, int G, bool ZERO>
 __global__ __launch_bounds__(kThreads, waves_of(TERMS, MT, G, ZERO)) void q4_kernel(Q4Args a, int chunk_steps, int rounds) {
     constexpr int kRows = 16 * MT, kGroups = kStep / G;
+    // The second terms lie in LDS 2^11 times as large.  Where the registers of 16 rows allow their products have sums of their own, which take that factor off
+    // where a group ends; else (forms of six waves a SIMD) the codes that they meet do, four instructions for 32 units.  Us, 1 row of V=65536 H=512, groups of 128:
+    // 9.2 / 9.5; 16 rows of V=200000 H=1024, groups of 64 with zero points 45.4 / 46.3.  The same for any number of rows, so that a row's sums are.
+    constexpr bool kApart = waves_of(TERMS, 1, G, ZERO) < 6 || (G == 128 && !ZERO);
+    constexpr bool kFirst = G == 64;                                    // the first terms' product first: the order that 80 registers hold
     extern __shared__ __attribute__((aligned(1024))) char lds[];        // [units of a chunk / 32][MT][TERMS][64 lanes][8]
     __shared__ uint32_t row_top[kRows];                                 // the row's largest finite magnitude
     __shared__ int row_exp[kRows];                                      // the power of two that it is divided by
@@ -195,7 +201,7 @@ __global__ __launch_bounds__(kThreads, waves_of(TERMS, MT, G, ZERO)) void q4_ker
         for (int s = 0; s < 8; ++s) {
             const float y = ldexpf(x[(s >> 1) + 4 * (s & 1)], -e);
             t1[s] = (_Float16)y;
-            t2[s] = (_Float16)(fabsf(y) < INFINITY ? y - (float)t1[s] : 0.f);       // (a NaN is in the first term)
+            t2[s] = (_Float16)(fabsf(y) < INFINITY ? 2048.f * (y - (float)t1[s]) : 0.f);       // (a NaN is in the first term)
         }
         *reinterpret_cast<f16x8 *>(lds + (size_t)frag * TERMS * 1024 + lane * 16) = t1;
         if (TERMS == 2) *reinterpret_cast<f16x8 *>(lds + (size_t)frag * 2048 + 1024 + lane * 16) = t2;
@@ -262,7 +268,7 @@ __global__ __launch_bounds__(kThreads, waves_of(TERMS, MT, G, ZERO)) void q4_ker
                 if (last >= a.codes && p > last) w = without(w, p - last < 16 ? (uint32_t)(p - last) : 16u);
             }
             if (G != kStep) w = transposed(w);
-            f32x4 part[MT];
+            f32x4 part[MT], rest[MT];
 #pragma unroll
             for (int t = 0; t < 4; ++t) {                               // 32 units each
                 constexpr int kPer = G / 32;
@@ -270,16 +276,22 @@ __global__ __launch_bounds__(kThreads, waves_of(TERMS, MT, G, ZERO)) void q4_ker
                 const uint32_t z = ZERO ? now.zero[grp] : 8u;
                 const f16x2 less = __builtin_bit_cast(f16x2, 0xE400E400u | z * 0x00010001u);
                 const f16x8 b = eight_codes(w[t], less, less + f16x2{(_Float16)960.f, (_Float16)960.f});
+                const f16x8 b2 = kApart ? b : b * (_Float16)0x1p-11f;
                 const float s = __uint_as_float(a.scale_bf16 ? now.scale[grp] << 16 : now.scale[grp]);
 #pragma unroll
                 for (int m = 0; m < MT; ++m) {
                     const char *at = lds + (size_t)((in_chunk * 4 + t) * MT + m) * TERMS * 1024 + lane * 16;
-                    if (t % kPer == 0) part[m] = f32x4{0.f, 0.f, 0.f, 0.f};
-                    if (TERMS == 2) part[m] = __builtin_amdgcn_mfma_f32_16x16x32_f16(*reinterpret_cast<const f16x8 *>(at + 1024), b, part[m], 0, 0, 0);
+                    if (t % kPer == 0) part[m] = rest[m] = f32x4{0.f, 0.f, 0.f, 0.f};
+                    f32x4 &to = kApart ? rest[m] : part[m];
+                    if (TERMS == 2 && !kFirst) to = __builtin_amdgcn_mfma_f32_16x16x32_f16(*reinterpret_cast<const f16x8 *>(at + 1024), b2, to, 0, 0, 0);
                     part[m] = __builtin_amdgcn_mfma_f32_16x16x32_f16(*reinterpret_cast<const f16x8 *>(at), b, part[m], 0, 0, 0);
+                    if (TERMS == 2 && kFirst) to = __builtin_amdgcn_mfma_f32_16x16x32_f16(*reinterpret_cast<const f16x8 *>(at + 1024), b2, to, 0, 0, 0);
                     if (t % kPer == kPer - 1)
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) acc[m][i] = __builtin_fmaf(s, part[m][i], acc[m][i]);
+                        for (int i = 0; i < 4; ++i) {
+                            const float sum = TERMS == 2 && kApart ? __builtin_fmaf(0x1p-11f, rest[m][i], part[m][i]) : part[m][i];
+                            acc[m][i] = __builtin_fmaf(s, sum, acc[m][i]);
+                        }
                 }
             }
             if (step + 1 == steps && v < a.V)
