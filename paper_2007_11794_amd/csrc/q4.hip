@@ -11,10 +11,11 @@
 // those four lanes (four register swaps) turns "32 units of one group per lane" into "the same group in all four lanes", so that a matrix
 // instruction never mixes two groups, whatever their size.  The A operand, the rows, lies in LDS in operand order, staged once per workgroup.
 //
-// What bounds it: V = 1048576, H = 1024, 1 row in 123 us is 4.6 TB/s, what a copy reaches.  Shorter launches (V = 200000, H = 1024, 16 rows, zero points 37
-// us, 3.2 TB/s; V = 65536, H = 512, 1 row 9.1 us) are the way to the first products (launch, rows to LDS and their magnitudes, 4 us), and
-// a last round of tiles that some waves have none of; a step costs a wave some 100 vector instructions for 2 KB of codes, half the time memory
-// takes for them.  Two tiles a wave, sharing the reads of the rows' operands, had fewer waves in flight: 47.2 us for the first of these.
+// What bounds it: V = 1048576, H = 1024, 1 row in bf16 in 117 us is 4.8 TB/s, what a copy reaches; in fp32, whose rows take twice the LDS and leave a compute
+// unit two workgroups of three, 158 us.  Shorter launches (V = 200000, H = 1024, 16 rows in bf16, zero points 37 us, 3.2 TB/s; V = 65536, H = 512, 1 row
+// 9.2 us) are the way to the first products (launch, rows to LDS and their magnitudes, 4 us), and a last round of tiles that some waves have none of; a
+// step costs a wave 75 to 120 vector instructions of four clocks for its 1 KB of codes, which memory takes some 460 clocks of the SIMD's for.  Two tiles a
+// wave, sharing the reads of the rows' operands, had fewer waves in flight: 47.3 us for the first of these when one took 42.3.
 #include "device_utils.h"
 #include "ops.h"
 
@@ -28,8 +29,8 @@ constexpr size_t kLdsRows = 144 * 1024;                      // most LDS for the
 constexpr int kHeld = 4;                                     // eights of a thread that wait in registers while the rows' magnitudes are found
 
 // Waves of a SIMD: six where their requests fit 80 registers, which is to say where there are few scales, no zero points, or rows of one term.  Us, four
-// waves / six: V = 1000000, H = 256, groups of 128, 1 row 42.8 / 37.9; H = 100, groups of 32, 8 rows 33.2 / 30.5; V = 200000, H = 1024, groups of 64 with
-// zero points, 16 rows in bf16 40.8 / 37, in fp32 44.6 / 45.7.
+// waves / six: V = 1000000, H = 256, groups of 128, 1 row 42.8 / 38.2; H = 100, groups of 32, 8 rows 34.3 / 31.8; V = 200000, H = 1024, groups of 64 with
+// zero points, 16 rows in bf16 40.8 / 37.5, in fp32 45.4 / 57.4.
 constexpr int waves_of(int TERMS, int MT, int G, bool zero) { return MT == 1 && (G == 128 || !zero || (G == 64 && TERMS == 1)) ? 6 : 4; }
 
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
@@ -208,7 +209,7 @@ __global__ __launch_bounds__(kThreads, waves_of(TERMS, MT, G, ZERO)) void q4_ker
     };
     // The power of two of every row: its largest finite magnitude goes to [2^14, 2^15).  Rows that are kHeld eights a thread are requested at
     // once and stay in registers meanwhile; of longer ones each eight is read for the magnitude and again.  (Read twice, 1 row of V = 65536, H = 1024
-    // took 15.4 us for 14.0, bf16 14.4 for 12.3.)
+    // took 16.0 us for 14.4, bf16 14.4 for 12.4.)
     const int units = steps * kStep, eights = units / 32 * MT * 64;
     const bool held = eights <= kHeld * kThreads && chunk_steps >= steps;
     Eight<TERMS == 1> x[kHeld];
@@ -364,8 +365,9 @@ template <int TERMS>
 hipError_t by_rows(const Q4Args &a, hipStream_t stream) {
     // Rows of a workgroup: 16 while all their tiles run at once (rows go to LDS by more workgroups), else 32; 64, whose operands need twice the
     // LDS, where every wave has several tiles and two such workgroups still share a compute unit's LDS and matrix cores (fp32 rows are two products
-    // each).  Us, 16 / 32 / 64 rows: 64 of V=2853 H=400 fp32 7.1 / 9.0 / 15.1; 40 of V=8000 H=1024 14.2 / 18.8 / 30.7; 64 of V=65536 H=512 26.2 / 23.3 / 28.4;
-    // bf16: 64 of V=65536 H=512 23.9 / 19.1 / 21.1; 512 of V=30000 H=512 82.5 / 57.2 / 47.8; 64 of V=100000 H=1024 48.0 / 42.2 / 48.2.
+    // each).  Us, 16 / 32 / 64 rows, groups of 64 with zero points: 64 of V=2853 H=400 fp32 7.0 / 8.8 / 16.2; 40 of V=8000 H=1024 13.2 / 19.3 / 32.2; 64 of V=65536
+    // H=512 25.4 / 21.4 / 30.1; 1024 of it 338 / 232 / 343; bf16: 64 of V=65536 H=512 21.7 / 17.0 / 19.8; 1024 of it 251 / 185 / 138; 512 of V=30000 H=512
+    // 59.4 / 46.2 / 40.0; 64 of V=100000 H=1024 55.2 / 48.0 / 58.6.
     const long long tiles = (a.V + 15) / 16, at_once = 2 * kChipGroups * kWaves;
     if (a.B <= 16 || (a.B + 15) / 16 * tiles <= at_once) return by_group<TERMS, 1>(a, stream);
     if (a.B > 32 && TERMS * TERMS * a.H <= 512 && (a.B + 63) / 64 * tiles >= 2 * at_once) return by_group<TERMS, 4>(a, stream);

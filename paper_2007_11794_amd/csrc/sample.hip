@@ -8,9 +8,11 @@
 // A row that fits the registers of one workgroup is read once.  Longer ones are cut into segments of that size for four small workgroups each,
 // and take four launches: maxima, histograms, the words of the deciding bin, the draw.
 //
-// What bounds it: weights in 64 bits, 17 double-precision instructions of eight clocks each and some ten others a word, 17 us for the 65536 words
-// of a compute unit, where a limit or the draw needs all of them; rows of small top_k need the weights of some hundred.  256 rows of 65536, us:
-// top_k and top_p 39, min_p 28, no limit 37, top_p alone 75 (17 of them LDS atomics and the kept words' weights once more), of which memory takes 14.
+// What bounds it: weights in 64 bits, 17 double-precision additions, products and multiply-adds of some five clocks of a SIMD with four waves, a maximum of nine
+// and ten other instructions a word, 12 us for one pass over the 65536 words of a compute unit, where a limit or the draw needs all of them; rows of small
+// top_k need the weights of some hundred.  256 rows of 65536, us: top_k and top_p 40, min_p 28, no limit 39, top_p alone 78 (two such passes, 14 of it the
+// kept words' weights for the draw, and an LDS atomic a word), of which memory takes 14.  The kernel of these rows is at the end of its registers: ten vector ones
+// and some seventy scalar ones are kept elsewhere, 44 bytes of scratch memory a lane.
 // Single precision would not do: a border between two of a million words moves by what the sum in front of it is off, and the word has to be the
 // definition's.
 #include "device_utils.h"
@@ -55,7 +57,7 @@ __device__ __forceinline__ double fma_with(double a, double b, double c) {
 // least relative error: with the rounding of its steps 3.3e-16 = 2^-51.4, so that a weight is off by less than one unit of 2^-50, whatever f.  (A degree less is good to
 // 1.5e-14, 17 of those units, two to 8.1e-13, and a border between two words moves by that share of the sum.)  Sums and products alone, at full rate: the nearest whole number
 // n comes of adding 1.5 * 2^52 and taking it off, its power of two goes into the exponent, and the result is rounded by adding 2^52, below which the last
-// bit counts 1 (with the instructions for rounding, conversion and scaling, a quarter of that rate each, 65536 weights took a workgroup 17.7 us for this).
+// bit counts 1 (with the instructions for rounding, conversion and scaling 256 rows of 65536 take 40.4 us for 38.4 without limits, 82.0 for 78.2 with top_p).
 __device__ __forceinline__ u64 fixed_exp2(double y, int bits) {
     y = fmax(y, -200.0);
     const double t = y + 0x1.8p52, f = y - (t - 0x1.8p52);
@@ -949,7 +951,7 @@ template <typename Z>
 hipError_t launch(const SampleArgs &a, int bits, hipStream_t stream) {
     const int vectors = (a.V + Row<Z>::E - 1) / Row<Z>::E;
     // Four waves a row for short rows, and for any that fit them where there are more rows than compute units.  Us, 256 threads / 1024: a row of 1000
-    // words 11.1 / 13.6; rows of 2853: 141 take 18.6 / 15.0, 600 take 21.3 / 32.0; 256 rows of 4000, top_p, 18.8 / 13.1.
+    // words 11.3 / 13.8; rows of 2853: 141 take 19.2 / 15.2, 600 take 21.7 / 32.5; 256 rows of 4000, top_p, 19.4 / 13.3.
     if (vectors <= 256 * 4 && (a.V < 2048 || a.N > kChipGroups)) return launch_row<Z, 256, 4>(a, bits, stream);
     if (vectors <= 1024 * 4) return launch_row<Z, 1024, 4>(a, bits, stream);
     if (vectors <= 1024 * 16) return launch_row<Z, 1024, 16>(a, bits, stream);
