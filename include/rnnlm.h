@@ -448,7 +448,7 @@ size_t rnnlm_distill_workspace_bytes(int N, int V);
  *   teacher_word   dev i32[N][K]  -1: no entry.  Repeated words add up.
  *   teacher_logit  dev f32[N][K]  -infinity: an entry of probability 0
  *   label          dev i32[N], -1: none; or NULL, with a = 0
- *   temperature    > 0, finite (below 2^-127 the shares are those at 2^-127);  label_weight in [0, 1]
+ *   temperature    > 0, finite (below 2^-126 the shares are those at 2^-126);  label_weight in [0, 1]
  *   row_weight     dev f32[N] or NULL: 1  (what the loss of a row weighs in the sum that is trained on)
  *   loss           dev f32[N] out, without row_weight
  *   stats          dev f32[N][4] out, for rnnlm_distill_backward: max z, 1 / sum exp((z - max) / T), 1 / sum exp(z - max), 0

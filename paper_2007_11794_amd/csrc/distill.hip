@@ -17,12 +17,17 @@ namespace rnnlm {
 
 namespace {
 
-// e^(x / T), per = log2(e) / T in two floats: what rounding the exponent's argument loses goes into a first-order term, so that shares
-// of any size are good to some 2^-22 of themselves.  (Below T = 2^-127 per would be infinite, and 0 times it NaN.)
+// Logits count by half their distance from the largest one: the whole of it may pass the range of a float, at temperatures where it still counts.  (One
+// instruction, as a difference, with the same rounding.)
+__device__ __forceinline__ float half_distance(float z, float half_top) { return __builtin_fmaf(0.5f, z, -half_top); }
+constexpr float kPer1 = 2.f * kLog2e;                        // 2 log2(e) / T at T = 1
+
+// e^(2 x / T) of half a distance x, per = 2 log2(e) / T in two floats: what rounding the exponent's argument loses goes into a first-order term, so that
+// shares of any size are good to some 2^-22 of themselves.  (Below T = 2^-126 per would be infinite, and 0 times it NaN.)
 struct Exponent {
     float per, rest;
     __device__ explicit Exponent(float T) {
-        const double c = 1.4426950408889634 / fmax((double)T, 0x1p-127);
+        const double c = 2 * 1.4426950408889634 / fmax((double)T, 0x1p-126);
         per = (float)c;
         rest = (float)(c - (double)per);
     }
@@ -156,49 +161,59 @@ struct List {
     }
 };
 
+// What a share at the temperature weighs in the gradient: row weight times (1 - a), k, times T.  (The product of the weights alone may pass the range of
+// a float.)
+__device__ __forceinline__ float soft_weight(const DistillArgs &a, float k, float share) { return (float)((double)k * (double)a.T * (double)share); }
+
 // The gradient of a row but for the teacher's words and the label.  TWO: shares at both temperatures, else those at one (`per`).
 template <bool TWO>
 struct RowGrad {
-    float top, per, c, c_1;        // weights times 1 / sums
-    bool dead;
-    __device__ RowGrad(const DistillArgs &a, float per_T, float top, float inv_T, float inv_1, float k_T, float k_1, bool bad) : top(top), per(per_T) {
-        dead = bad || ((k_T != 0.f || k_1 != 0.f) && inv_T != inv_T);
-        c = dead ? quiet_nan() : k_T != 0.f ? k_T * inv_T : 0.f;
+    float half_top, per, c, c_1;   // weights times 1 / sums
+    bool dead, nothing;
+    __device__ RowGrad(const DistillArgs &a, float per_T, float top, float inv_T, float inv_1, float k, float k_1, bool bad) : half_top(0.5f * top), per(per_T) {
+        dead = bad || ((k != 0.f || k_1 != 0.f) && inv_T != inv_T);
+        nothing = !dead && k == 0.f && k_1 == 0.f;
+        c = dead ? quiet_nan() : k != 0.f ? soft_weight(a, k, inv_T) : 0.f;
         c_1 = !dead && k_1 != 0.f ? k_1 * inv_1 : 0.f;
-        if (!TWO && c_1 != 0.f) { c = k_T != 0.f ? c + c_1 : c_1; per = kLog2e; }      // (both only at T = 1)
+        if (!TWO && k_1 != 0.f) { c += c_1; per = kPer1; }    // (both only at T = 1)
     }
-    __device__ __forceinline__ bool nothing() const { return c == 0.f && c_1 == 0.f; }
     __device__ __forceinline__ float operator()(float z) const {
-        const float d = z - top;
+        const float d = half_distance(z, half_top);
         const float r = c * fast_exp2(d * per);
-        return TWO ? __builtin_fmaf(c_1, fast_exp2(d * kLog2e), r) : r;
+        return TWO ? __builtin_fmaf(c_1, fast_exp2(d * kPer1), r) : r;
     }
 };
 
 // The places of the teacher's words and of the label within [from, from + len) of the row, written over what is there.  `in_list`: the label
 // is one of the words.  Called behind a barrier that awaited the stores.
 template <typename Z, int THREADS, typename Grad>
-__device__ __forceinline__ void write_listed(const DistillArgs &a, const List &list, const Grad &grad, Z *out, int from, int len, float k_T, float k_1, bool repeats,
+__device__ __forceinline__ void write_listed(const DistillArgs &a, const List &list, const Grad &grad, Z *out, int from, int len, float k, float k_1, bool repeats,
                                              int label, float z_label) {
     bool mine = false;
-    for (int k = threadIdx.x; k_T != 0.f && k < list.K; k += THREADS) {
-        const int w = list.word[k];
+    for (int i = threadIdx.x; k != 0.f && i < list.K; i += THREADS) {
+        const int w = list.word[i];
         if (w < from || w >= from + len) continue;
         mine |= w == label;
-        const float q = list.share_of(k, repeats);
-        if (q >= 0.f) Row<Z>::put(out + w, grad(list.z[k]) - k_T * q - (w == label ? k_1 : 0.f));
+        const float q = list.share_of(i, repeats);
+        if (q >= 0.f) Row<Z>::put(out + w, grad(list.z[i]) - soft_weight(a, k, q) - (w == label ? k_1 : 0.f));
     }
     const bool in_list = __syncthreads_or(mine);
     if (threadIdx.x == 0 && !in_list && label >= from && label < from + len && k_1 != 0.f) Row<Z>::put(out + label, grad(z_label) - k_1);
 }
 
-// Loss of a row: soft = T sum q (log q - log p), the label's -log p.  (That sum grows as 1 / T and T^2 passes the range of a float far in front of
-// what their product is.)
-__device__ __forceinline__ float row_loss(const DistillArgs &a, bool bad, bool soft_part, bool hard_part, bool dead, float soft, float hard) {
+// The soft part of a row's loss, (1 - a) T^2 sum q (log q - log p), is held in units of T^2, below T = 1 of 2 T: the sum grows as 1 / T, and T^2 passes
+// the range of a float far in front of what their product is.
+struct SoftUnits {
+    float distance, log;           // of half a distance, and of a logarithm
+    __device__ explicit SoftUnits(const DistillArgs &a)
+        : distance(a.T < 1.f ? 1.f - a.a : 2.f * (1.f - a.a) / a.T), log(a.T < 1.f ? 0.5f * a.T * (1.f - a.a) : 1.f - a.a) {}
+};
+// Loss of a row: `soft` in those units; the label's -log p is log_sum less twice z_label, half its distance.
+__device__ __forceinline__ float row_loss(const DistillArgs &a, bool bad, bool soft_part, bool hard_part, bool dead, float soft, float log_sum, float z_label) {
     if (bad || ((soft_part || hard_part) && dead)) return quiet_nan();
     float l = 0.f;
-    if (soft_part) l = (1.f - a.a) * (a.T * soft);
-    if (hard_part) l += a.a * hard;
+    if (soft_part) l = a.T < 1.f ? (2.f * a.T) * soft : a.T * (a.T * soft);
+    if (hard_part) l += a.a * log_sum - 2.f * a.a * z_label;
     return l;
 }
 
@@ -238,14 +253,14 @@ __global__ __launch_bounds__(THREADS, 4) void distill_row_kernel(DistillArgs a, 
     for (int r = 0; r < R; ++r)
 #pragma unroll
         for (int j = 0; j < E; ++j) mine = fmaxf(mine, Row<Z>::get(v[r], j));
-    float from = mine == -INFINITY ? 0.f : mine;
+    float from = mine == -INFINITY ? 0.f : 0.5f * mine;
     float at_T[E] = {}, at_1[E] = {};
     auto add = [&](u32x4 x) {
 #pragma unroll
         for (int j = 0; j < E; ++j) {
-            const float d = Row<Z>::get(x, j) - from;
+            const float d = half_distance(Row<Z>::get(x, j), from);
             at_T[j] += fast_exp2(d * per);
-            if (FORM != kOne) at_1[j] += fast_exp2(d * kLog2e);
+            if (FORM != kOne) at_1[j] += fast_exp2(d * kPer1);
         }
     };
 #pragma unroll
@@ -253,8 +268,8 @@ __global__ __launch_bounds__(THREADS, 4) void distill_row_kernel(DistillArgs a, 
         forget(v[r]);
         add(v[r]);
     }
-    at_T[0] += fast_exp2((z_tail - from) * per);
-    if (FORM != kOne) at_1[0] += fast_exp2((z_tail - from) * kLog2e);
+    at_T[0] += fast_exp2(half_distance(z_tail, from) * per);
+    if (FORM != kOne) at_1[0] += fast_exp2(half_distance(z_tail, from) * kPer1);
     // What does not stay in registers, four vectors on their way at a time.  The first STASH of a thread stay in LDS.
     for (int f = 0; R * THREADS + f * THREADS < vectors; f += 4) {
         u32x4 x[4];
@@ -271,17 +286,18 @@ __global__ __launch_bounds__(THREADS, 4) void distill_row_kernel(DistillArgs a, 
 #pragma unroll
             for (int j = 0; j < E; ++j) high = fmaxf(high, Row<Z>::get(x[q], j));
             if (high > mine) {
-                const float by_T = fast_exp2((mine - high) * per), by_1 = fast_exp2((mine - high) * kLog2e);
+                const float d = half_distance(mine, 0.5f * high), by_T = fast_exp2(d * per), by_1 = fast_exp2(d * kPer1);
 #pragma unroll
                 for (int j = 0; j < E; ++j) { at_T[j] *= by_T; at_1[j] *= by_1; }
-                from = mine = high;
+                mine = high;
+                from = 0.5f * high;
             }
             add(x[q]);
         }
     }
     float m[2] = {t_mine, mine};
     block_reduce<2, true, WAVES>(m, part);                  // (also: the list is there)
-    const float t_top = m[0], top = m[1];
+    const float t_top = m[0], half_t_top = 0.5f * t_top, top = m[1], half_top = 0.5f * top;
     const bool bad = t_top == INFINITY || label < -1 || label >= V;
     const bool soft_part = t_top > -INFINITY && a.a < 1.f, hard_part = label >= 0 && a.a > 0.f;
     for (int k = tid; k < a.K; k += THREADS) {
@@ -294,36 +310,37 @@ __global__ __launch_bounds__(THREADS, 4) void distill_row_kernel(DistillArgs a, 
 #pragma unroll
         for (int i = 0; i < j; ++i) { at_T[i] += at_T[i + j]; at_1[i] += at_1[i + j]; }
     // (a thread without a finite logit has sums of 0, or of NaN; the row's own maximum is infinite or there is nothing where `top` is)
-    const float down = mine > -INFINITY ? mine - top : 0.f;
-    float s[3] = {at_T[0] * fast_exp2(down * per), at_1[0] * fast_exp2(down * kLog2e), 0.f};
+    const float down = mine > -INFINITY ? half_distance(mine, half_top) : 0.f;
+    float s[3] = {at_T[0] * fast_exp2(down * per), at_1[0] * fast_exp2(down * kPer1), 0.f};
     for (int k = tid; k < a.K; k += THREADS)
-        if (list.word[k] >= 0) s[2] += exponent.fine(list.q[k] - t_top);
+        if (list.word[k] >= 0) s[2] += exponent.fine(half_distance(list.q[k], half_t_top));
     block_reduce<3, false, WAVES>(s, part);
     const float s_T = s[0], s_1 = FORM == kOne ? s[0] : s[1], t_sum = s[2];
     const bool dead = !(s_T > 0.f);                         // a NaN, +infinity, or nothing finite
     const float inv_T = dead ? quiet_nan() : 1.f / s_T, inv_1 = dead ? quiet_nan() : 1.f / s_1;
     float l[1] = {0.f};
     if (soft_part && !bad) {
+        const SoftUnits units(a);
         const float log_sum = logf(s_T), log_t = logf(t_sum);
         for (int k = tid; k < a.K; k += THREADS) {
             if (list.word[k] < 0) continue;
-            const float d = list.q[k] - t_top, q = exponent.fine(d) / t_sum;
-            if (q > 0.f) l[0] += q * (d - (list.z[k] - top) + a.T * (log_sum - log_t));
+            const float d = half_distance(list.q[k], half_t_top), q = exponent.fine(d) / t_sum;
+            if (q > 0.f) l[0] += q * ((d - half_distance(list.z[k], half_top)) * units.distance + (log_sum - log_t) * units.log);
             list.q[k] = q;
         }
     }
     block_reduce<1, false, WAVES>(l, part);
     if (tid == 0) {
-        a.loss[n] = row_loss(a, bad, soft_part, hard_part, dead, l[0], logf(s_1) - (z_label - top));
+        a.loss[n] = row_loss(a, bad, soft_part, hard_part, dead, l[0], logf(s_1), half_distance(z_label, half_top));
         *reinterpret_cast<f32x4_any *>(a.stats + 4ll * n) = f32x4{top, inv_T, inv_1, 0.f};
     }
     if (!GRAD) return;
     const float g = a.row_weight ? a.row_weight[n] : 1.f;
-    const float k_T = soft_part ? g * (1.f - a.a) * a.T : 0.f, k_1 = hard_part ? g * a.a : 0.f;
-    const RowGrad<FORM == kTwo> grad(a, per, top, inv_T, inv_1, k_T, k_1, bad);
+    const float k = soft_part ? g * (1.f - a.a) : 0.f, k_1 = hard_part ? g * a.a : 0.f;
+    const RowGrad<FORM == kTwo> grad(a, per, top, inv_T, inv_1, k, k_1, bad);
     Z *out = static_cast<Z *>(a.grad) + n * a.grad_ld;
     const int at = forget(tid);
-    if (grad.nothing()) {                                   // nothing is learned from the row, whatever it holds
+    if (grad.nothing) {                                   // nothing is learned from the row, whatever it holds
         const float zeros[E] = {};
         for (int i = tid; i < vectors; i += THREADS) store_vector(out, i, zeros);
         store_tail(out, V, 0.f);
@@ -361,13 +378,13 @@ __global__ __launch_bounds__(THREADS, 4) void distill_row_kernel(DistillArgs a, 
     const bool again = list.repeated<THREADS>();
     seen_by_all();
     const bool repeats = __syncthreads_or(again);
-    write_listed<Z, THREADS>(a, list, grad, out, 0, V, k_T, k_1, repeats, label, z_label);
+    write_listed<Z, THREADS>(a, list, grad, out, 0, V, k, k_1, repeats, label, z_label);
 }
 
 // ---- rows in segments
 constexpr int kSegThreads = kDistillThreads, kSegWaves = kSegThreads / 64, kMaxSegments = 64;
-// Of one segment: maximum m, sums relative to it at both temperatures, sum of q (z - m) and of q over the teacher's words in it, the label's
-// z - m.
+// Of one segment: maximum m, sums relative to it at both temperatures, sum of q (z - m) / 2 and of q over the teacher's words in it, the label's
+// (z - m) / 2.
 struct Part { float m, s_T, s_1, qz, q, label, pad[2]; };
 
 template <typename Z>
@@ -391,27 +408,27 @@ __global__ __launch_bounds__(kSegThreads) void distill_part_kernel(DistillArgs a
         for (int j = 0; j < E; ++j) m[1] = fmaxf(m[1], Row<Z>::get(x, j));
     }
     block_reduce<2, true, WAVES>(m, part);
-    const float t_top = m[0], top = m[1];
+    const float t_top = m[0], half_t_top = 0.5f * t_top, top = m[1], half_top = 0.5f * top;
     const bool listed = t_top > -INFINITY && t_top < INFINITY;
     float at_T[E] = {}, at_1[E] = {};
     for (int i = tid; i < vectors; i += kSegThreads) {
         const u32x4 x = load_vector(row + from, i);
 #pragma unroll
         for (int j = 0; j < E; ++j) {
-            const float z = Row<Z>::get(x, j), d = z == -INFINITY ? -INFINITY : z - top;     // (top may be -infinity itself here)
+            const float z = Row<Z>::get(x, j), d = z == -INFINITY ? -INFINITY : half_distance(z, half_top);     // (half_top may be -infinity itself here)
             at_T[j] += fast_exp2(d * per);
-            at_1[j] += fast_exp2(d * kLog2e);
+            at_1[j] += fast_exp2(d * kPer1);
         }
     }
 #pragma unroll
     for (int j = E / 2; j; j /= 2)
 #pragma unroll
         for (int i = 0; i < j; ++i) { at_T[i] += at_T[i + j]; at_1[i] += at_1[i + j]; }
-    const float d_tail = z_tail == -INFINITY ? -INFINITY : z_tail - top;
-    float s[5] = {at_T[0] + fast_exp2(d_tail * per), at_1[0] + fast_exp2(d_tail * kLog2e), 0.f, 0.f, 0.f};
+    const float d_tail = z_tail == -INFINITY ? -INFINITY : half_distance(z_tail, half_top);
+    float s[5] = {at_T[0] + fast_exp2(d_tail * per), at_1[0] + fast_exp2(d_tail * kPer1), 0.f, 0.f, 0.f};
     if (listed)
         for (int k = tid; k < a.K; k += kSegThreads)
-            if (list.word[k] >= 0) s[2] += exponent.fine(list.q[k] - t_top);
+            if (list.word[k] >= 0) s[2] += exponent.fine(half_distance(list.q[k], half_t_top));
     block_reduce<5, false, WAVES>(s, part);
     const float t_sum = s[2];
     float d[2] = {0.f, 0.f};
@@ -419,13 +436,13 @@ __global__ __launch_bounds__(kSegThreads) void distill_part_kernel(DistillArgs a
         for (int k = tid; k < a.K; k += kSegThreads) {
             const int w = list.word[k];
             if (w < from || w >= from + len) continue;
-            const float q = exponent.fine(list.q[k] - t_top) / t_sum, z = Row<Z>::one(row + w);
-            if (q > 0.f) { d[0] += q * (z == -INFINITY ? -INFINITY : z - top); d[1] += q; }
+            const float q = exponent.fine(half_distance(list.q[k], half_t_top)) / t_sum, z = Row<Z>::one(row + w);
+            if (q > 0.f) { d[0] += q * (z == -INFINITY ? -INFINITY : half_distance(z, half_top)); d[1] += q; }
         }
     block_reduce<2, false, WAVES>(d, part);
     if (tid == 0) {
         Part p = {top, s[0], s[1], d[0], d[1], 0.f, {0.f, 0.f}};
-        if (label >= from && label < from + len) { const float z = Row<Z>::one(row + label); p.label = z == -INFINITY ? -INFINITY : z - top; }
+        if (label >= from && label < from + len) { const float z = Row<Z>::one(row + label); p.label = z == -INFINITY ? -INFINITY : half_distance(z, half_top); }
         static_cast<Part *>(a.ws)[blockIdx.x] = p;
     }
 }
@@ -459,19 +476,20 @@ __global__ __launch_bounds__(kSegThreads) void distill_segment_kernel(DistillArg
     for (int k = tid; k < a.K; k += kSegThreads) {
         const int w = list.word[k];
         if (w < 0 || bad) continue;
-        s[0] += exponent.fine(list.q[k] - t_top);
+        s[0] += exponent.fine(half_distance(list.q[k], 0.5f * t_top));
         if (w >= from && w < from + len) list.z[k] = Row<Z>::one(row + w);
     }
     const float z_label = !bad && label >= from && label < from + len ? Row<Z>::one(row + label) : 0.f;
     block_reduce<1, false, WAVES>(s, part);
     const float t_sum = s[0];
+    const SoftUnits units(a);
     float entropy[1] = {0.f};
     if (soft_part && !bad) {
         const float log_t = logf(t_sum);
         for (int k = tid; k < a.K; k += kSegThreads) {
             if (list.word[k] < 0) continue;
-            const float d = list.q[k] - t_top, q = exponent.fine(d) / t_sum;
-            if (q > 0.f) entropy[0] += q * (d - a.T * log_t);
+            const float d = half_distance(list.q[k], 0.5f * t_top), q = exponent.fine(d) / t_sum;
+            if (q > 0.f) entropy[0] += q * (d * units.distance - log_t * units.log);
             list.q[k] = q;
         }
     }
@@ -485,27 +503,27 @@ __global__ __launch_bounds__(kSegThreads) void distill_segment_kernel(DistillArg
         if (lane < parts) p = static_cast<const Part *>(a.ws)[(long long)n * parts + lane];
         top = wave_max(p.m);
         const bool some = p.m > -INFINITY;
-        const float d = p.m - top;
-        const float s_T = wave_sum(some ? p.s_T * fast_exp2(d * per) : p.s_T), s_1 = wave_sum(some ? p.s_1 * fast_exp2(d * kLog2e) : p.s_1);
+        const float d = half_distance(p.m, 0.5f * top);
+        const float s_T = wave_sum(some ? p.s_T * fast_exp2(d * per) : p.s_T), s_1 = wave_sum(some ? p.s_1 * fast_exp2(d * kPer1) : p.s_1);
         const bool dead = !(s_T > 0.f) || top == INFINITY;
         inv_T = dead ? quiet_nan() : 1.f / s_T;
         inv_1 = dead ? quiet_nan() : 1.f / s_1;
         if (seg == 0) {
             block_reduce<1, false, WAVES>(entropy, part);
             const float qz = wave_sum(p.q > 0.f ? p.qz + p.q * d : 0.f), q = wave_sum(p.q);
-            const float z_minus = wave_sum(hard_part && !bad && label / part_len == lane ? p.label + (some ? d : 0.f) : 0.f);
+            const float z_half = wave_sum(hard_part && !bad && label / part_len == lane ? p.label + (some ? d : 0.f) : 0.f);
             if (tid == 0) {
-                a.loss[n] = row_loss(a, bad, soft_part, hard_part, dead, entropy[0] - qz + q * (a.T * logf(s_T)), logf(s_1) - z_minus);
+                a.loss[n] = row_loss(a, bad, soft_part, hard_part, dead, entropy[0] - qz * units.distance + q * (logf(s_T) * units.log), logf(s_1), z_half);
                 *reinterpret_cast<f32x4_any *>(a.stats + 4ll * n) = f32x4{top, inv_T, inv_1, 0.f};
             }
         }
     }
     if (len == 0) return;
     const float g = a.row_weight ? a.row_weight[n] : 1.f;
-    const float k_T = soft_part ? g * (1.f - a.a) * a.T : 0.f, k_1 = hard_part ? g * a.a : 0.f;
-    const RowGrad<TWO> grad(a, per, top, inv_T, inv_1, k_T, k_1, bad);
+    const float k = soft_part ? g * (1.f - a.a) : 0.f, k_1 = hard_part ? g * a.a : 0.f;
+    const RowGrad<TWO> grad(a, per, top, inv_T, inv_1, k, k_1, bad);
     Z *out = static_cast<Z *>(a.grad) + n * a.grad_ld + from;
-    if (grad.nothing()) {
+    if (grad.nothing) {
         const float zeros[E] = {};
         for (int i = tid; i < vectors; i += kSegThreads) store_vector(out, i, zeros);
         store_tail(out, len, 0.f);
@@ -527,7 +545,7 @@ __global__ __launch_bounds__(kSegThreads) void distill_segment_kernel(DistillArg
     const bool again = list.repeated<kSegThreads>();
     seen_by_all();
     const bool repeats = __syncthreads_or(again);
-    write_listed<Z, kSegThreads>(a, list, grad, out - from, from, len, k_T, k_1, repeats, label, z_label);
+    write_listed<Z, kSegThreads>(a, list, grad, out - from, from, len, k, k_1, repeats, label, z_label);
 }
 
 int hash_size_of(int K) {

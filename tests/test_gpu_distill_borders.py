@@ -41,3 +41,27 @@ def test_temperatures_of_any_size(N, V, T):
             wanted[n] = want
         check(d, T, a, wanted, grad, rows=range(0, N, 10))
         check(d, T, a, wanted, backward(d, T, a, stats), rows=range(0, N, 10))
+
+
+@pytest.mark.parametrize("T", [0.5, 1.0, 2e37, 1e38, 3e38])
+@pytest.mark.parametrize("N,V,dtype", [(6, 3000, torch.float32), (6, 3000, torch.bfloat16), (2, 70001, torch.float32), (60, 70001, torch.float32), (20, 140000, torch.bfloat16)])
+def test_logits_further_apart_than_the_largest_number(N, V, dtype, T):
+    """Shares at such temperatures are of order one; a loss beyond the largest float is infinite."""
+    t = float(np.float32(T))
+    rng = np.random.default_rng(V)
+    d = case(N, V, 40, dtype)
+    d["z"] = torch.from_numpy((rng.uniform(-1, 1, (N, V)) * 3.3e38).astype(np.float32)).to(DEV).to(dtype)
+    d["t"] = torch.from_numpy((rng.uniform(-1, 1, (N, 40)) * 3.3e38).astype(np.float32)).to(DEV)
+    rows = range(0, N, 10)
+    for a in (0.0, 0.25, 1.0):
+        loss, stats, grad = run(d, T, a)
+        only = run(d, T, a, grad=False)[0]
+        wanted = torch.full((N,), np.nan, dtype=torch.float64)
+        for n in rows:
+            want, _, far = distill_row(d["z"][n].double().cpu().numpy(), d["words"][n].cpu().numpy(), d["t"][n].double().cpu().numpy(), int(d["label"][n]), t, a)
+            bar = (t * t * (1 - a) + a) * (2.0 ** -18 + (V / 256 + 16) * 2.0 ** -24 + 2.0 ** -20 * far) + 2.0 ** -22 * abs(want)
+            for got in (float(loss[n]), float(only[n])):
+                assert got == np.inf if want - bar > 3.4028235e38 else abs(got - want) <= bar or (got == np.inf and want + bar > 3.4028235e38), (n, a, got, want)
+            wanted[n] = want
+        check(d, T, a, wanted, grad, rows=rows)
+        check(d, T, a, wanted, backward(d, T, a, stats), rows=rows)
