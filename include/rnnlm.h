@@ -388,6 +388,7 @@ int rnnlm_pack_ids(const uint32_t *ctx_idx, const uint32_t *small_lm_idx, int N,
  * Codes less their zero are exact; an fp32 x is taken as two fp16 terms relative to its row's largest finite magnitude (good to
  * 2^-23 of itself or 2^-50 of that magnitude, whichever is larger), a bf16 x as it is (where it is below 2^-31 of that magnitude, to
  * 2^-39 of it); sums are held in fp32, and y is rounded once at the end.
+ * Scales are to be below 2^88 in magnitude: sums are held relative to the row's largest x, and larger ones may pass the range of a float.
  * An x that is infinite or NaN reaches the outputs of its row as in exact arithmetic (infinity times a zero weight is NaN),
  * and no other row.  B = 0 is a no-op.  H <= 65536, V <= 2^30, B <= 2^24 (RNNLM_ERANGE).
  */
